@@ -270,6 +270,72 @@ int caat_block_bwd(const caat_desc* d, const void* const* weights, const void* x
                    void* workspace, size_t ws_bytes, const void* dx_out, const void* dr_out, void* dx, void* dr,
                    void* const* dweights, float* dgamma, float* dbeta, void* hip_stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Serving over a paged key / value cache.  The sequences of a batch have lengths of their own, and the memory of their keys
+ * and values is handed out in pages.  Keys and values lie in two pools per rank, of n_pages pages of page_size positions
+ * each; page_table [batch][max_pages] (int32, shared by the ranks: every rank's pool uses the same page numbers) names the
+ * page of position p of sequence b at column p / page_size.  The new tokens of all sequences are packed into rows, the same
+ * for every rank:
+ *   row_start [batch + 1] int32 : sequence b owns rows row_start[b] .. row_start[b + 1] - 1, none if they are equal.  NULL:
+ *                                 sequence b owns row b (one new token each, b < rows)
+ *   lens [batch] int32          : positions of sequence b in the cache WITH its new tokens; with n of them, the i-th sits at
+ *                                 position lens[b] - n + i
+ * Both, and the table, are read on the device, so a captured call follows them from replay to replay.  What they hold is
+ * checked there: a sequence whose rows are not inside 0 .. rows (or end before they begin) has none, a negative length is
+ * none, a table entry outside 0 .. n_pages - 1, or a position at or behind max_pages * page_size, is no page: nothing is
+ * written there, and its keys are not seen.  A page may stand in the tables of several sequences (a common beginning);
+ * two tokens of one call must not be appended to the same place.  Rows that belong to no sequence are left as they are.
+ */
+typedef enum caat_cache {
+  CAAT_CACHE_BF16 = 0,
+  CAAT_CACHE_E4M3 = 1   /* OCP e4m3 codes of value / scale, one fp32 scale per (rank, key / value head) and cache; rounded to
+                           nearest even, beyond +-448 the largest code, NaN stays NaN */
+} caat_cache;
+
+typedef struct caat_paged_desc {
+  int T;                /* ranks */
+  int batch;            /* sequences (rows of page_table) */
+  int n_heads, n_kv_heads; /* over all ranks, as in caat_desc (n_kv_heads 0: n_heads) */
+  int head_dim;         /* 128 (CAAT_EUNSUPPORTED otherwise) */
+  int cache_type;       /* caat_cache */
+  int page_size;        /* positions per page, a multiple of 16 */
+  int max_pages;        /* columns of page_table */
+  long long n_pages;    /* pages of a rank's pool */
+  long long rows;       /* token rows per rank of qkv, q and out */
+  int max_new;          /* the most new tokens a sequence has in these calls: chooses the kernel, results do not depend on it
+                           beyond their rounding */
+  float rope_base;      /* caat_paged_append: > 0 */
+  long long ld_qkv, ld_q; /* elements from row to row of qkv and q; 0: packed.  Ranks lie rows * ld apart */
+  long long stride_rank, stride_page, stride_head, stride_row; /* of both caches, in elements, multiples of 16; all 0:
+                           [T][n_pages][n_kv_heads / T][page_size][128].  Any order of pages, heads and positions whose 128
+                           channels are contiguous; 16 * stride_row elements must stay below 2 GiB */
+} caat_paged_desc;
+
+/*
+ * Rotary embedding of the new tokens and the store of their keys and values.  qkv [T, rows, hd_r + 2*kvd_r] holds the
+ * un-rotated projections q | k | v (see caat_block_fwd), pairs (j, j + 64) turn by position * rope_base^(-2j/128); the angle is
+ * good to 1e-6 at any position below 2^24.
+ *   q_out [T, rows, hd_r]: the rotated queries.  May be qkv itself with ld_q = ld_qkv (rotation in place; k and v of qkv
+ *   keep their values) and must not overlap it otherwise.
+ *   k_scale, v_scale: [T][n_kv_heads / T] fp32, CAAT_CACHE_E4M3 only (CAAT_EINVAL otherwise); positive and finite; NULL: 1
+ */
+int caat_paged_append(const caat_paged_desc* d, const void* qkv, void* q_out, const int* row_start, const int* lens,
+                      const int* page_table, void* k_cache, void* v_cache, const float* k_scale, const float* v_scale,
+                      void* hip_stream);
+
+/*
+ * Causal attention of the new tokens over the pages of their sequences (their own keys are read from the cache, so they are
+ * appended first): out[row of token i of b, head] = sum_t softmax_t(q . k_t / sqrt(128)) v_t over positions
+ * t <= lens[b] - n + i.  q [T, rows, hd_r] with rotated queries, out [T, rows, hd_r] packed.  A row that sees no key, or whose
+ * scores are all minus infinity, is zeros.  Nothing that lies in a page behind its sequence's length takes part, whatever it
+ * holds.  workspace: caat_paged_attn_workspace_bytes(d) bytes, which depends neither on the lengths nor on max_pages;
+ * nothing in it has to be kept or cleared between calls.
+ */
+size_t caat_paged_attn_workspace_bytes(const caat_paged_desc* d);
+int caat_paged_attn(const caat_paged_desc* d, const void* q, void* out, const int* row_start, const int* lens,
+                    const int* page_table, const void* k_cache, const void* v_cache, const float* k_scale,
+                    const float* v_scale, void* workspace, size_t ws_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,6 +19,7 @@ OK, EINVAL, ESHAPE, EALIGN, EWORKSPACE, EHIP, EUNSUPPORTED, ESCRATCH = range(8)
 MLP_GELU, MLP_SWIGLU, ATTN, ATTN_DECODE, LAYER_PREFILL = range(5)
 LAYERNORM, RMSNORM = 0, 1
 GEMM_NT, GEMM_NN, GEMM_TN = 0, 1, 2
+CACHE_BF16, CACHE_E4M3 = 0, 1
 
 
 class CaatError(RuntimeError):
@@ -35,6 +36,14 @@ class caat_desc(C.Structure):
                 ("reduce_in_gemm", C.c_int), ("dedup_shared", C.c_int), ("separate_reduce", C.c_int)]
 
 
+class caat_paged_desc(C.Structure):
+    _fields_ = [("T", C.c_int), ("batch", C.c_int), ("n_heads", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int),
+                ("cache_type", C.c_int), ("page_size", C.c_int), ("max_pages", C.c_int), ("n_pages", C.c_longlong),
+                ("rows", C.c_longlong), ("max_new", C.c_int), ("rope_base", C.c_float), ("ld_qkv", C.c_longlong),
+                ("ld_q", C.c_longlong), ("stride_rank", C.c_longlong), ("stride_page", C.c_longlong),
+                ("stride_head", C.c_longlong), ("stride_row", C.c_longlong)]
+
+
 class caat_ws_layout(C.Structure):
     _fields_ = [(n, C.c_size_t) for n in (
         "total_bytes", "off_P", "bytes_P", "off_Y", "bytes_Y", "off_mean", "bytes_mean", "off_rstd", "bytes_rstd",
@@ -45,7 +54,8 @@ class caat_ws_layout(C.Structure):
 # the method's C ABI (include/caat.h) and the measuring tools the library exports beside it (csrc/caat_tools.h)
 EXPORTS = ["caat_shared_channels", "caat_status_string", "caat_workspace_bytes", "caat_workspace_layout",
            "caat_partial_sync", "caat_norm_fwd", "caat_partial_sync_norm_fwd", "caat_norm_bwd_workspace_bytes",
-           "caat_norm_bwd", "caat_norm_bwd_static", "caat_gemm_bf16", "caat_block_fwd", "caat_block_bwd"]
+           "caat_norm_bwd", "caat_norm_bwd_static", "caat_gemm_bf16", "caat_block_fwd", "caat_block_bwd",
+           "caat_paged_append", "caat_paged_attn_workspace_bytes", "caat_paged_attn"]
 TOOL_EXPORTS = ["caat_profile_enable", "caat_profile_reset", "caat_profile_count", "caat_profile_get", "caat_hbm_probe",
                 "caat_gemm_route", "caat_gemm_pair_route",
                 "caat_gemm_shared_pair_route"]
@@ -88,6 +98,13 @@ def lib() -> C.CDLL:
         L.caat_block_bwd.argtypes = [C.POINTER(caat_desc), C.POINTER(vp), vp, vp, vp, sz, vp, vp, vp, vp,
                                      C.POINTER(vp), vp, vp, vp]
         L.caat_block_bwd.restype = i
+        pd = C.POINTER(caat_paged_desc)
+        L.caat_paged_append.argtypes = [pd, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.caat_paged_append.restype = i
+        L.caat_paged_attn_workspace_bytes.argtypes = [pd]
+        L.caat_paged_attn_workspace_bytes.restype = sz
+        L.caat_paged_attn.argtypes = [pd, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.caat_paged_attn.restype = i
         L.caat_profile_enable.argtypes = [i]
         L.caat_profile_enable.restype = i
         L.caat_profile_reset.argtypes = []
@@ -267,6 +284,40 @@ def block_bwd(desc: caat_desc, weights: Sequence, x, r_out, workspace, dx_out, d
                               _ptr(dbeta), _stream(stream))
     if check:
         _check(st, "caat_block_bwd")
+    return st
+
+
+def paged_desc(T: int, batch: int, n_heads: int, rows: int, page_size: int, n_pages: int, max_pages: int, max_new: int = 1,
+               n_kv_heads: int = 0, head_dim: int = 128, cache_type: int = CACHE_BF16, rope_base: float = 10000.0, ld_qkv: int = 0,
+               ld_q: int = 0, strides: Sequence[int] = (0, 0, 0, 0)) -> caat_paged_desc:
+    """strides: (rank, page, head, row) of both caches in elements; zeros: [T][n_pages][n_kv_heads / T][page_size][128]."""
+    return caat_paged_desc(T=T, batch=batch, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, cache_type=cache_type,
+                           page_size=page_size, max_pages=max_pages, n_pages=n_pages, rows=rows, max_new=max_new,
+                           rope_base=rope_base, ld_qkv=ld_qkv, ld_q=ld_q, stride_rank=strides[0], stride_page=strides[1],
+                           stride_head=strides[2], stride_row=strides[3])
+
+
+def paged_append(desc: caat_paged_desc, qkv, q_out, row_start, lens, page_table, k_cache, v_cache, k_scale=None, v_scale=None,
+                 stream=None, check: bool = True) -> int:
+    st = lib().caat_paged_append(C.byref(desc), _ptr(qkv), _ptr(q_out), _ptr(row_start), _ptr(lens), _ptr(page_table),
+                                 _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _stream(stream))
+    if check:
+        _check(st, "caat_paged_append")
+    return st
+
+
+def paged_attn_workspace_bytes(desc: caat_paged_desc) -> int:
+    return lib().caat_paged_attn_workspace_bytes(C.byref(desc))
+
+
+def paged_attn(desc: caat_paged_desc, q, out, row_start, lens, page_table, k_cache, v_cache, workspace, k_scale=None,
+               v_scale=None, stream=None, check: bool = True) -> int:
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    st = lib().caat_paged_attn(C.byref(desc), _ptr(q), _ptr(out), _ptr(row_start), _ptr(lens), _ptr(page_table),
+                               _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(workspace), ws_bytes,
+                               _stream(stream))
+    if check:
+        _check(st, "caat_paged_attn")
     return st
 
 

@@ -530,6 +530,52 @@ int layer_fwd(const caat_desc* d, const caat_ws_layout& L, const void* const* we
   return CAAT_OK;
 }
 
+// ---- paged cache: the checks that both of its calls share, and the kernels' arguments
+int paged_args(const caat_paged_desc* d, const int* row_start, const int* lens, const int* page_table, const float* k_scale,
+               const float* v_scale, PagedArgs* a) {
+  if (!d || d->T < 1 || d->batch < 1 || d->rows < 0 || d->n_pages < 0 || d->max_new < 1) return CAAT_EINVAL;
+  if (d->cache_type != CAAT_CACHE_BF16 && d->cache_type != CAAT_CACHE_E4M3) return CAAT_EINVAL;
+  if (d->n_heads < 1 || d->n_kv_heads < 0 || d->head_dim < 1 || d->max_pages < 1 || d->page_size < 1) return CAAT_EINVAL;
+  if (d->cache_type != CAAT_CACHE_E4M3 && (k_scale || v_scale)) return CAAT_EINVAL;
+  const int kv = d->n_kv_heads > 0 ? d->n_kv_heads : d->n_heads;
+  if (d->n_heads % d->T != 0 || d->n_heads % kv != 0 || kv % d->T != 0) return CAAT_ESHAPE;
+  if (d->head_dim != 128) return CAAT_EUNSUPPORTED;
+  constexpr long long MAX = 0x7FFFFFFFLL;
+  if (d->page_size % 16 != 0 || (long long)d->max_pages * d->page_size > MAX || d->n_pages > MAX) return CAAT_ESHAPE;
+  if (!row_start && d->batch > d->rows) return CAAT_ESHAPE;
+  const long long hpr = d->n_heads / d->T, kvpr = kv / d->T;
+  const long long hd = hpr * 128, qw = hd + 2 * kvpr * 128;
+  const long long st[4] = {d->stride_rank, d->stride_page, d->stride_head, d->stride_row};
+  const bool plain = !st[0] && !st[1] && !st[2] && !st[3];
+  if (!plain) {
+    for (long long x : st)
+      if (x < 0 || x % 16 != 0) return CAAT_ESHAPE;
+    if (st[3] < 128 || st[3] >= (MAX + 1) / 32) return CAAT_ESHAPE;
+  }
+  if ((d->ld_q && (d->ld_q < hd || d->ld_q % 8 != 0)) || (d->ld_qkv && (d->ld_qkv < qw || d->ld_qkv % 8 != 0))) return CAAT_ESHAPE;
+  // grids and row numbers are 32-bit
+  if (d->rows > MAX || d->rows * hpr > MAX || (long long)d->T * hpr > 65535 || hpr > 32768 || (long long)d->batch * d->T * hpr > MAX)
+    return CAAT_ESHAPE;
+  a->row_start = row_start;
+  a->lens = lens;
+  a->table = page_table;
+  a->k_scale = k_scale;
+  a->v_scale = v_scale;
+  a->T = d->T; a->batch = d->batch; a->hpr = (int)hpr; a->kvpr = (int)kvpr;
+  a->page_size = d->page_size; a->max_pages = d->max_pages; a->rows = (int)d->rows; a->n_pages = d->n_pages;
+  a->ld_q = d->ld_q ? d->ld_q : hd;
+  a->s_row = plain ? 128 : st[3];
+  a->s_head = plain ? (long long)d->page_size * 128 : st[2];
+  a->s_page = plain ? kvpr * a->s_head : st[1];
+  a->s_rank = plain ? d->n_pages * a->s_page : st[0];
+  return CAAT_OK;
+}
+inline bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+bool paged_misaligned(const PagedArgs& a, const void* k_cache, const void* v_cache) {
+  return misaligned(k_cache) || misaligned(v_cache) || misaligned4(a.row_start) || misaligned4(a.lens) || misaligned4(a.table) ||
+         misaligned4(a.k_scale) || misaligned4(a.v_scale);
+}
+
 }  // namespace
 
 extern "C" {
@@ -798,6 +844,46 @@ int caat_block_fwd(const caat_desc* d, const void* const* weights, const void* x
                         d->norm, (int)T, n, (int)h, d->eps, s, dedup_hs(d));
   }
   return hip_status(e);
+}
+
+int caat_paged_append(const caat_paged_desc* d, const void* qkv, void* q_out, const int* row_start, const int* lens,
+                      const int* page_table, void* k_cache, void* v_cache, const float* k_scale, const float* v_scale,
+                      void* hip_stream) {
+  PagedArgs a;
+  const int st = paged_args(d, row_start, lens, page_table, k_scale, v_scale, &a);
+  if (st != CAAT_OK) return st;
+  if (d->rows == 0) return CAAT_OK;   // buffers without elements may have no address
+  if (!qkv || !q_out || !lens || !page_table || !k_cache || !v_cache || !(d->rope_base > 0.0f)) return CAAT_EINVAL;
+  if (misaligned(qkv) || misaligned(q_out) || paged_misaligned(a, k_cache, v_cache)) return CAAT_EALIGN;
+  const long long ld_qkv = d->ld_qkv ? d->ld_qkv : (long long)(a.hpr + 2 * a.kvpr) * 128;
+  if (q_out == qkv && a.ld_q != ld_qkv) return CAAT_ESHAPE;
+  ProfScope ps((hipStream_t)hip_stream, "paged_append");
+  return hip_status(launch_paged_append(a, d->cache_type == CAAT_CACHE_E4M3, (const bf16_t*)qkv, (bf16_t*)q_out, ld_qkv, k_cache,
+                                        v_cache, d->rope_base, (hipStream_t)hip_stream));
+}
+
+size_t caat_paged_attn_workspace_bytes(const caat_paged_desc* d) {
+  PagedArgs a;
+  static const int some = 0;   // stands for a table of rows: a batch may have sequences without any
+  if (paged_args(d, &some, nullptr, nullptr, nullptr, nullptr, &a) != CAAT_OK) return 0;
+  return paged_attn_workspace_bytes(a.T, a.hpr, a.kvpr, a.rows);
+}
+
+int caat_paged_attn(const caat_paged_desc* d, const void* q, void* out, const int* row_start, const int* lens,
+                    const int* page_table, const void* k_cache, const void* v_cache, const float* k_scale,
+                    const float* v_scale, void* workspace, size_t ws_bytes, void* hip_stream) {
+  PagedArgs a;
+  const int st = paged_args(d, row_start, lens, page_table, k_scale, v_scale, &a);
+  if (st != CAAT_OK) return st;
+  if (d->rows == 0) return CAAT_OK;
+  const size_t need = paged_attn_workspace_bytes(a.T, a.hpr, a.kvpr, a.rows);
+  if (!q || !out || !lens || !page_table || !k_cache || !v_cache || (need > 0 && !workspace)) return CAAT_EINVAL;
+  if (misaligned(q) || misaligned(out) || paged_misaligned(a, k_cache, v_cache) || (need > 0 && misaligned(workspace)))
+    return CAAT_EALIGN;
+  if (ws_bytes < need) return CAAT_EWORKSPACE;
+  ProfScope ps((hipStream_t)hip_stream, "paged_attn");
+  return hip_status(launch_paged_attn(a, d->cache_type == CAAT_CACHE_E4M3, (const bf16_t*)q, (bf16_t*)out, k_cache, v_cache,
+                                      d->max_new, workspace, (hipStream_t)hip_stream));
 }
 
 int caat_block_bwd(const caat_desc* d, const void* const* weights, const void* x, const void* r_out, void* workspace,

@@ -378,4 +378,21 @@ hipError_t launch_decode_attn(const bf16_t* qkv, bf16_t* kc, bf16_t* vc, bf16_t*
                               int d, long long cap, long long nkeys, float rope_base, void* scratch, size_t scratch_bytes,
                               hipStream_t s);
 
+// ---------------------------------------------------------------- paged key / value cache
+struct PagedArgs {
+  const int* row_start;   // may be null: sequence b owns row b
+  const int* lens;
+  const int* table;       // [batch][max_pages]
+  const float* k_scale;   // [T][kvpr] or null
+  const float* v_scale;
+  int T, batch, hpr, kvpr, page_size, max_pages;
+  int rows;
+  long long n_pages, ld_q, s_rank, s_page, s_head, s_row;   // elements
+};
+hipError_t launch_paged_append(const PagedArgs& a, int e4m3, const bf16_t* qkv, bf16_t* q_out, long long ld_qkv, void* kc, void* vc,
+                               float rope_base, hipStream_t s);
+size_t paged_attn_workspace_bytes(int T, int hpr, int kvpr, long long rows);
+hipError_t launch_paged_attn(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, int max_new,
+                             void* workspace, hipStream_t s);
+
 }  // namespace caat

@@ -1,0 +1,213 @@
+// Paged key / value cache for gfx950: the new tokens of a ragged batch are rotated and stored to the pages of their sequences,
+// and attend to them.
+#include <math.h>
+#include "caat_internal.h"
+
+namespace caat {
+
+static constexpr int PHD = 128;                  // head dim
+
+// Rows of sequence b: the first and how many; none unless they lie inside the packed rows.
+__device__ __forceinline__ int seq_rows(const PagedArgs& a, int b, int& first) {
+  if (!a.row_start) {
+    first = b;
+    return b < a.rows ? 1 : 0;
+  }
+  const int r0 = a.row_start[b], r1 = a.row_start[b + 1];
+  first = r0;
+  return r0 >= 0 && r1 > r0 && r1 <= a.rows ? r1 - r0 : 0;
+}
+
+// The sequence that owns a row (the first one, -1: none); called by whole waves, the answer is uniform.
+__device__ __forceinline__ int seq_of_row(const PagedArgs& a, int row, int& first, int& n) {
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    int f = 0, m = 0;
+    if (b0 + lane < a.batch) m = seq_rows(a, b0 + lane, f);
+    const unsigned long long hit = __ballot(m > 0 && row >= f && row < f + m);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      first = __shfl(f, l, 64);
+      n = __shfl(m, l, 64);
+      return b0 + l;
+    }
+  }
+  return -1;
+}
+
+__device__ __forceinline__ float e4m3_clamp(float x) { return x != x ? x : fminf(fmaxf(x, -448.0f), 448.0f); }
+// eight values to eight e4m3 codes
+__device__ __forceinline__ uint2 pack_e4m3(const float* v) {
+  uint2 w;
+  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_clamp(v[0]), e4m3_clamp(v[1]), 0, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_clamp(v[2]), e4m3_clamp(v[3]), lo, true);
+  int hi = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_clamp(v[4]), e4m3_clamp(v[5]), 0, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_clamp(v[6]), e4m3_clamp(v[7]), hi, true);
+  w.x = (unsigned)lo;
+  w.y = (unsigned)hi;
+  return w;
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// Append.  A workgroup owns a row on all ranks (or, of few rows, every gridDim.y-th part of its heads): the row's 64 sines and
+// cosines are made once, then a thread turns 8 pairs (j, j + 64) of one q or k head at a time and moves the matching channels
+// of v along with k.
+struct RopeTable {
+  float2 rev[64];   // revolutions per position: base^(-2j/128) / (2 pi), from 64 bits, in two floats
+};
+
+template <bool E4M3>
+__global__ __launch_bounds__(256) void paged_append_kernel(const PagedArgs a, const RopeTable rt, const bf16_t* qkv, bf16_t* q_out,
+                                                           long long ld_qkv, void* kc, void* vc) {
+  __shared__ float s_cs[64], s_sn[64];
+  const int row = blockIdx.x, tid = threadIdx.x;
+  int first, n;
+  const int b = seq_of_row(a, row, first, n);
+  if (b < 0) return;
+  const int pos = max(a.lens[b], 0) - n + (row - first);
+  if (tid < 64) {
+    float sn, cs;
+    rope_sincos((float)pos, rt.rev[tid], sn, cs);
+    s_cs[tid] = cs;
+    s_sn[tid] = sn;
+  }
+  __syncthreads();
+  const int col = pos / a.page_size;
+  const int page = pos >= 0 && col < a.max_pages ? a.table[(long long)b * a.max_pages + col] : -1;
+  const bool store = page >= 0 && page < a.n_pages;
+  const long long slot = (long long)page * a.s_page + (long long)(pos - col * a.page_size) * a.s_row;
+  const int per = (a.hpr + a.kvpr) * 8;
+  for (int u = blockIdx.y * 256 + tid; u < a.T * per; u += gridDim.y * 256) {
+    const int rank = u / per, rem = u - rank * per;
+    const int head = rem >> 3, grp = rem & 7;
+    const bf16_t* src = qkv + ((long long)rank * a.rows + row) * ld_qkv + head * PHD + grp * 8;
+    const uint4 lo = *reinterpret_cast<const uint4*>(src), hi = *reinterpret_cast<const uint4*>(src + 64);
+    const unsigned lw[4] = {lo.x, lo.y, lo.z, lo.w}, hw[4] = {hi.x, hi.y, hi.z, hi.w};
+    float y1[8], y2[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x1 = e & 1 ? hi_bf(lw[e >> 1]) : lo_bf(lw[e >> 1]), x2 = e & 1 ? hi_bf(hw[e >> 1]) : lo_bf(hw[e >> 1]);
+      const float cs = s_cs[grp * 8 + e], sn = s_sn[grp * 8 + e];
+      y1[e] = x1 * cs - x2 * sn;
+      y2[e] = x2 * cs + x1 * sn;
+    }
+    const bool is_k = head >= a.hpr;
+    if (!is_k || !E4M3) {
+      const uint4 r1 = make_uint4(pack2bf(y1[0], y1[1]), pack2bf(y1[2], y1[3]), pack2bf(y1[4], y1[5]), pack2bf(y1[6], y1[7]));
+      const uint4 r2 = make_uint4(pack2bf(y2[0], y2[1]), pack2bf(y2[2], y2[3]), pack2bf(y2[4], y2[5]), pack2bf(y2[6], y2[7]));
+      bf16_t* dst = is_k ? (bf16_t*)kc + rank * a.s_rank + slot + (head - a.hpr) * a.s_head + grp * 8
+                         : q_out + ((long long)rank * a.rows + row) * a.ld_q + head * PHD + grp * 8;
+      if (!is_k || store) {
+        *reinterpret_cast<uint4*>(dst) = r1;
+        *reinterpret_cast<uint4*>(dst + 64) = r2;
+      }
+    }
+    if (is_k && store) {
+      const int kvh = head - a.hpr;
+      const uint4 vlo = *reinterpret_cast<const uint4*>(src + a.kvpr * PHD), vhi = *reinterpret_cast<const uint4*>(src + a.kvpr * PHD + 64);
+      const long long at = rank * a.s_rank + slot + kvh * a.s_head + grp * 8;
+      if constexpr (E4M3) {
+        const float ki = a.k_scale ? 1.0f / a.k_scale[rank * a.kvpr + kvh] : 1.0f, vi = a.v_scale ? 1.0f / a.v_scale[rank * a.kvpr + kvh] : 1.0f;
+        const unsigned vw[8] = {vlo.x, vlo.y, vlo.z, vlo.w, vhi.x, vhi.y, vhi.z, vhi.w};
+        float v[16];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          y1[e] *= ki;
+          y2[e] *= ki;
+          v[2 * e] = lo_bf(vw[e]) * vi;
+          v[2 * e + 1] = hi_bf(vw[e]) * vi;
+        }
+        unsigned char *k8 = (unsigned char*)kc + at, *v8 = (unsigned char*)vc + at;
+        *reinterpret_cast<uint2*>(k8) = pack_e4m3(y1);
+        *reinterpret_cast<uint2*>(k8 + 64) = pack_e4m3(y2);
+        *reinterpret_cast<uint2*>(v8) = pack_e4m3(v);
+        *reinterpret_cast<uint2*>(v8 + 64) = pack_e4m3(v + 8);
+      } else {
+        *reinterpret_cast<uint4*>((bf16_t*)vc + at) = vlo;
+        *reinterpret_cast<uint4*>((bf16_t*)vc + at + 64) = vhi;
+      }
+    }
+  }
+}
+
+hipError_t launch_paged_append(const PagedArgs& a, int e4m3, const bf16_t* qkv, bf16_t* q_out, long long ld_qkv, void* kc, void* vc,
+                               float rope_base, hipStream_t s) {
+  if (a.rows == 0) return hipSuccess;
+  RopeTable rt;
+  for (int j = 0; j < 64; ++j) {
+    const double rev = exp2(-2.0 * j / PHD * log2((double)rope_base)) / 6.283185307179586476925;
+    rt.rev[j].x = (float)rev;
+    rt.rev[j].y = (float)(rev - (double)rt.rev[j].x);
+  }
+  const int units = a.T * (a.hpr + a.kvpr) * 8;
+  const int parts = a.rows < 512 ? (units + 255) / 256 : 1;
+  const dim3 grid((unsigned)a.rows, (unsigned)parts);
+  if (e4m3) hipLaunchKernelGGL(paged_append_kernel<true>, grid, dim3(256), 0, s, a, rt, qkv, q_out, ld_qkv, kc, vc);
+  else hipLaunchKernelGGL(paged_append_kernel<false>, grid, dim3(256), 0, s, a, rt, qkv, q_out, ld_qkv, kc, vc);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// Attention, the simple form: a wave owns one (rank, row, query head) and walks the keys it sees, two channels per lane.
+template <bool E4M3>
+__device__ __forceinline__ float2 ld_pair(const void* base, long long at) {   // channels at, at + 1
+  if constexpr (E4M3) {
+    const unsigned w = *reinterpret_cast<const unsigned short*>((const unsigned char*)base + at);
+    const auto f = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
+    return make_float2(f[0], f[1]);
+  } else {
+    const unsigned w = *reinterpret_cast<const unsigned*>((const bf16_t*)base + at);
+    return make_float2(lo_bf(w), hi_bf(w));
+  }
+}
+template <bool E4M3>
+__global__ __launch_bounds__(256) void paged_attn_simple_kernel(const PagedArgs a, const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
+                                                                const void* __restrict__ kc, const void* __restrict__ vc, float scale_log2) {
+  const int lane = threadIdx.x & 63;
+  const int row = blockIdx.x, u = blockIdx.y * 4 + (threadIdx.x >> 6);
+  int first, n;
+  const int b = seq_of_row(a, row, first, n);
+  if (b < 0 || u >= a.T * a.hpr) return;
+  const int rank = u / a.hpr, head = u - rank * a.hpr, kvh = head / (a.hpr / a.kvpr);
+  const long long cap = (long long)a.max_pages * a.page_size;
+  const long long seen = min((long long)max(a.lens[b], 0) - n + (row - first) + 1, cap);
+  const unsigned qw = *reinterpret_cast<const unsigned*>(q + ((long long)rank * a.rows + row) * a.ld_q + head * PHD + lane * 2);
+  const float q0 = lo_bf(qw), q1 = hi_bf(qw);
+  if (a.k_scale) scale_log2 *= a.k_scale[rank * a.kvpr + kvh];
+  float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+  for (long long t = 0; t < seen; ++t) {
+    const long long col = t / a.page_size;
+    const int page = a.table[b * (long long)a.max_pages + col];
+    if (page < 0 || page >= a.n_pages) continue;
+    const long long at = rank * a.s_rank + page * a.s_page + kvh * a.s_head + (t - col * a.page_size) * a.s_row + lane * 2;
+    const float2 k = ld_pair<E4M3>(kc, at), v = ld_pair<E4M3>(vc, at);
+    float sc = q0 * k.x + q1 * k.y;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sc += __shfl_xor(sc, off, 64);
+    sc *= scale_log2;
+    const float m_new = fmaxf(m, sc), base = m_new == -INFINITY ? 0.0f : m_new;
+    const float alpha = exp2f(m - base), p = exp2f(sc - base);
+    l = l * alpha + p;
+    o0 = o0 * alpha + p * v.x;
+    o1 = o1 * alpha + p * v.y;
+    m = m_new;
+  }
+  const float inv = l == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[rank * a.kvpr + kvh] : 1.0f) / l;
+  *reinterpret_cast<unsigned*>(out + ((long long)rank * a.rows + row) * a.hpr * PHD + head * PHD + lane * 2) = pack2bf(o0 * inv, o1 * inv);
+}
+
+size_t paged_attn_workspace_bytes(int, int, int, long long) { return 0; }
+
+hipError_t launch_paged_attn(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, int max_new,
+                             void* workspace, hipStream_t s) {
+  (void)max_new;
+  (void)workspace;
+  if (a.rows == 0) return hipSuccess;
+  const float scale_log2 = 1.4426950408889634f / sqrtf((float)PHD);
+  const dim3 grid((unsigned)a.rows, (unsigned)((a.T * a.hpr + 3) / 4));
+  if (e4m3) hipLaunchKernelGGL(paged_attn_simple_kernel<true>, grid, dim3(256), 0, s, a, q, out, kc, vc, scale_log2);
+  else hipLaunchKernelGGL(paged_attn_simple_kernel<false>, grid, dim3(256), 0, s, a, q, out, kc, vc, scale_log2);
+  return hipGetLastError();
+}
+
+}  // namespace caat

@@ -1,0 +1,211 @@
+"""Append to and attention over a paged key / value cache, against the definition in 64 bits, through the C ABI."""
+import numpy as np
+import pytest
+
+from paper_2506_19645_amd import binding as B
+from tests import paged_util as P
+
+pytestmark = pytest.mark.gpu
+
+# T, heads, kv_heads, lens, news, page, e4m3, order
+FEW_TOKENS = [
+    (1, 1, 1, [1], [1], 16, False, "phrd"),
+    (2, 4, 4, [37], [1], 16, False, "phrd"),
+    (1, 4, 1, [15, 16, 17, 31, 32, 33, 0, 1], [1, 1, 1, 1, 1, 1, 0, 1], 16, False, "phrd"),
+    (2, 16, 4, [300, 1, 511, 64], [1, 1, 1, 1], 64, False, "prhd"),          # [page][position][head]
+    (1, 40, 2, [77, 129], [1, 1], 48, False, "hprd"),                        # groups of 20 heads: more than one tile of rows
+    (2, 2, 2, [2000, 3, 700], [1, 1, 1], 80, False, "phrd"),
+    (1, 8, 2, [100, 9, 0, 260], [5, 9, 0, 4], 16, False, "phrd"),            # drafts; 9 new of 9
+    (1, 2, 2, [64, 200], [17, 3], 32, False, "phrd"),                        # 17 rows
+    (1, 3, 1, [50, 4], [5, 4], 16, False, "phrd"),                           # 15 and 12 rows
+    (1, 1, 1, [1], [1], 16, True, "phrd"),
+    (2, 8, 2, [15, 16, 17, 31, 32, 33, 0, 1], [1, 1, 1, 1, 1, 1, 0, 1], 16, True, "phrd"),
+    (1, 8, 1, [300, 1, 511, 64], [1, 2, 3, 2], 48, True, "prhd"),
+    (2, 2, 2, [2000, 3, 700], [1, 1, 1], 32, True, "phrd"),
+    (4, 64, 8, [1500], [1], 256, True, "hprd"),
+]
+PROMPTS = [
+    (1, 2, 2, [128], [128], 16, False, "phrd"),
+    (2, 4, 2, [63, 64, 65], [63, 64, 65], 16, False, "phrd"),
+    (1, 2, 1, [129, 1, 0, 300], [129, 1, 0, 40], 64, False, "prhd"),
+    (1, 6, 2, [500, 333], [257, 91], 48, False, "hprd"),                     # groups of 3 heads: tokens across tiles
+    (1, 1, 1, [700], [33], 80, False, "phrd"),
+    (2, 8, 2, [200, 77], [200, 50], 16, True, "phrd"),
+    (1, 3, 1, [500, 2, 90], [257, 2, 90], 48, True, "prhd"),
+    (1, 2, 2, [1000], [130], 128, True, "phrd"),
+]
+
+
+@pytest.mark.parametrize("T,heads,kv,lens,news,page,e4m3,order", FEW_TOKENS + PROMPTS)
+def test_append(T, heads, kv, lens, news, page, e4m3, order):
+    c = P.make(11, T, heads, kv, lens, news, page, e4m3, order, pad_rows=2)
+    d = P.on_gpu(c)
+    k0, v0 = c.k.copy(), c.v.copy()
+    P.append(c, d)
+    P.check_append(c, P.bits(d.q_out), P.bits(d.k), P.bits(d.v), k0, v0)
+
+
+@pytest.mark.parametrize("T,heads,kv,lens,news,page,e4m3,order", FEW_TOKENS)
+def test_attention_of_few_tokens(T, heads, kv, lens, news, page, e4m3, order):
+    c = P.make(12, T, heads, kv, lens, news, page, e4m3, order, pad_rows=2)
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.FEW)
+
+
+@pytest.mark.parametrize("T,heads,kv,lens,news,page,e4m3,order", PROMPTS)
+def test_attention_of_prompts(T, heads, kv, lens, news, page, e4m3, order):
+    c = P.make(13, T, heads, kv, lens, news, page, e4m3, order, pad_rows=2)
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.MANY)
+
+
+def test_append_far_positions_and_wide_rows():
+    """Positions up to 2^24 - 1 (the angle is carried beyond fp32), rows of qkv and q wider than their heads, other base."""
+    far = [2 ** 24 - 16, 1000003, 131071]
+    c = P.make(14, 1, 4, 2, [3, 2, 1], [3, 2, 1], 16, ld_q=4 * 128 + 40, ld_qkv=8 * 128 + 8)
+    c.lens[:] = far                                      # behind every column of the table: rotated, and stored nowhere
+    d = P.on_gpu(c)
+    P.append(c, d)
+    P.check_append(c, P.bits(d.q_out), P.bits(d.k), P.bits(d.v), c.k, c.v)
+    c.desc.rope_base = 500000.0
+    d = P.on_gpu(c)
+    P.append(c, d)
+    q, qs = P.ref_append(c, 500000.0)[:2]
+    got, own = P.widen(P.bits(d.q_out)), ~np.isnan(q)
+    assert np.all((np.abs(got - q) <= 2.0 ** -8 * np.abs(q) + 6e-6 * qs)[own])
+
+
+def test_append_in_place():
+    """q rotated where it lies: the same bits as into a buffer of its own, k and v of the rows as they were."""
+    c = P.make(15, 2, 8, 2, [40, 9], [7, 3], 16)
+    d, e = P.on_gpu(c), P.on_gpu(c)
+    P.append(c, d)
+    c.desc.ld_q = c.ld_qkv
+    B.paged_append(c.desc, e.qkv, e.qkv, e.row_start, e.lens, e.table, e.k, e.v)
+    got = P.bits(e.qkv)
+    assert np.array_equal(got[:, :, :c.hpr * 128], P.bits(d.q_out)) and np.array_equal(got[:, :, c.hpr * 128:], c.qkv[:, :, c.hpr * 128:])
+    assert np.array_equal(P.bits(e.k), P.bits(d.k)) and np.array_equal(P.bits(e.v), P.bits(d.v))
+
+
+def test_append_e4m3_ends_of_the_range():
+    """Beyond +-448 the largest code, NaN stays NaN, halves go to even, the smallest codes are there; scale 1 where none is given."""
+    c = P.make(16, 1, 1, 1, [1], [1], 16, True, scales=False)
+    vals = np.zeros(128, dtype=np.float32)
+    vals[:12] = [1000.0, -1e30, np.inf, -np.inf, np.nan, 17.0, 19.0, 2.0 ** -9, 2.0 ** -10, 3 * 2.0 ** -10, 448.0, 464.0]
+    c.qkv[0, 0, 256:] = P.bf16(vals)
+    c.qkv[0, 0, 260] = 0x7FC0
+    d = P.on_gpu(c)
+    d.ks = d.vs = None
+    P.append(c, d)
+    got = P.decode(P.view(c, P.bits(d.v))[0, c.table[0, 0], 0, 0], True)
+    want = np.zeros(128)
+    want[:12] = [448, -448, 448, -448, np.nan, 16, 20, 2.0 ** -9, 0, 2 * 2.0 ** -9, 448, 448]
+    assert np.array_equal(got, want, equal_nan=True)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("new", [1, 3, 150])
+def test_what_no_query_sees_does_not_matter(e4m3, new):
+    """NaN and infinities behind a sequence's length, in pages of nobody and in pages that are masked; lengths that end inside
+    a page."""
+    lens = [new + 5, new + 27, new + 48]
+    c = P.make(17, 1, 4, 2, lens, [new] * 3, 32, e4m3)
+    used = np.zeros((c.n_pages, c.page), dtype=bool)
+    for b, x in enumerate(lens):
+        for t in range(x):
+            used[c.table[b, t // c.page], t % c.page] = True
+    for x in (c.k, c.v):
+        w = P.view(c, x)
+        bad = [0x7F, 0xFF] if e4m3 else [0x7FC0, 0xFF80, 0x7F80, 0xFFFF]
+        fill = np.resize(np.array(bad, dtype=x.dtype), w.shape)
+        w[:, ~used.any(axis=1)] = fill[:, ~used.any(axis=1)]
+        for page, off in zip(*np.where(~used)):
+            w[:, page, :, off] = fill[:, page, :, off]
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.FEW if new <= 3 else P.MANY)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("new", [1, 2, 90])
+def test_lists_that_are_wrong(e4m3, new):
+    """Entries that are no page, lengths below the number of new tokens, negative or behind the table, rows outside the packed
+    ones: nothing outside is read or written, and what is left is computed."""
+    lens = [new + 100, new + 40, new + 33, new + 64, new + 20, new + 7]
+    c = P.make(18, 2, 4, 2, lens, [new] * 6, 16, e4m3, pad_rows=1)
+    c.table[0, 2], c.table[0, 4] = -1, c.n_pages         # holes in the middle
+    c.table[1, :] = 2 ** 31 - 1                          # no page at all
+    c.lens[2] = new - 1                                  # its first token sits in front of position 0
+    c.lens[3] = -5
+    c.lens[4] = c.table.shape[1] * c.page + 3            # behind the last column
+    c.table[4, :] = c.table[5, 0]
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.FEW if new <= 2 else P.MANY)
+    c.table[4, :] = -1                                   # (two tokens must not be appended to one place)
+    d = P.on_gpu(c)
+    P.append(c, d)
+    P.check_append(c, P.bits(d.q_out), P.bits(d.k), P.bits(d.v), c.k, c.v)
+    for wrong in ([-1, new, 2 * new, 3 * new, 4 * new, 5 * new, 6 * new], [0, new, new - 1, 2 ** 31 - 1, 4 * new, 4 * new, 6 * new + 2]):
+        d = P.on_gpu(c)
+        import torch
+        d.row_start = torch.tensor(wrong, dtype=torch.int32, device="cuda")
+        P.append(c, d)
+        P.attend(c, d)
+        got = P.widen(P.bits(d.out))
+        owned = np.zeros(c.rows, dtype=bool)
+        for r0, r1 in zip(wrong[:-1], wrong[1:]):
+            if 0 <= r0 < r1 <= c.rows:
+                owned[r0:r1] = True
+        assert np.all(got[:, ~owned] == -7.0) and np.all(np.isfinite(got))
+
+
+def test_without_a_list_of_rows():
+    """row_start NULL: sequence b owns row b, the rows behind the last sequence nobody's."""
+    c = P.make(19, 2, 8, 4, [33, 0, 200, 16], [1, 1, 1, 1], 16, pad_rows=3)
+    ref, size = P.ref_attn(c)
+    d = P.on_gpu(c)
+    d.row_start = None
+    P.attend(c, d)
+    P.check_attn(c, P.bits(d.out), ref, size, P.FEW)
+    P.append(c, d)
+    P.check_append(c, P.bits(d.q_out), P.bits(d.k), P.bits(d.v), c.k, c.v)
+
+
+def test_no_rows():
+    c = P.make(20, 1, 2, 2, [40, 3], [0, 0], 16)
+    d = P.on_gpu(c)
+    P.append(c, d)
+    P.attend(c, d)
+    assert np.all(P.widen(P.bits(d.out)) == -7.0) and np.array_equal(P.bits(d.k), c.k)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_a_batch_that_grows_step_by_step(e4m3):
+    """Prompts are appended and attended, then tokens one by one and two by two, pages handed out on the way: every output is
+    that of the definition over what the caches hold, and what they hold is what the definition appends."""
+    import torch
+    T, heads, kv, page = 2, 8, 2, 16
+    steps = [[70, 1, 33], [1, 1, 1], [1, 2, 1], [0, 14, 1], [2, 0, 2]]
+    total = [sum(s[b] for s in steps) for b in range(3)]
+    whole = P.make(21, T, heads, kv, total, total, page, e4m3)
+    k, v, ws = None, None, None
+    lens = [0, 0, 0]
+    for i, news in enumerate(steps):
+        lens = [x + n for x, n in zip(lens, news)]
+        c = P.make(30 + i, T, heads, kv, lens, news, page, e4m3, spare=0, columns=whole.table.shape[1])
+        c.n_pages, c.table, c.ks, c.vs = whole.n_pages, whole.table.copy(), whole.ks, whole.vs
+        for b, x in enumerate(lens):
+            c.table[b, -(-x // page):] = -1
+        c.desc.n_pages = whole.n_pages
+        c.desc.stride_rank, c.desc.stride_page = whole.desc.stride_rank, whole.desc.stride_page
+        c.k, c.v = (whole.k, whole.v) if k is None else (k, v)
+        d = P.on_gpu(c)
+        P.append(c, d)
+        P.attend(c, d, q=d.q_out)
+        k, v = P.bits(d.k).copy(), P.bits(d.v).copy()
+        P.check_append(c, P.bits(d.q_out), k, v, c.k, c.v)
+        c.k, c.v = k, v
+        P.check_attn(c, P.bits(d.out), *P.ref_attn(c, q=P.bits(d.q_out)), P.MANY)
