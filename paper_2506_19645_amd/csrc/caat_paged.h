@@ -1,0 +1,34 @@
+// What the kernels over a paged key / value cache share (device code).
+#pragma once
+#include "caat_internal.h"
+
+namespace caat {
+
+static constexpr int PHD = 128;                  // head dim
+
+// Rows of sequence b: the first and how many; none unless they lie inside the packed rows.
+__device__ __forceinline__ int seq_rows(const PagedArgs& a, int b, int& first) {
+  if (!a.row_start) {
+    first = b;
+    return b < a.rows ? 1 : 0;
+  }
+  const int r0 = a.row_start[b], r1 = a.row_start[b + 1];
+  first = r0;
+  return r0 >= 0 && r1 > r0 && r1 <= a.rows ? r1 - r0 : 0;
+}
+
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long long uni64(long long x) {
+  return (long long)(((unsigned long long)(unsigned)uni((int)(x >> 32)) << 32) | (unsigned)uni((int)x));
+}
+__device__ __forceinline__ long long lane64(long long x, int lane) {   // a lane's value, `lane` uniform
+  return (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32) |
+                     (unsigned)__builtin_amdgcn_readlane((int)x, lane));
+}
+
+// The two forms of the attention.  `few`: a query tile is 16 (token, head of the group) rows, see caat_paged_few.hip
+size_t paged_few_workspace_bytes();
+hipError_t launch_paged_few(const PagedArgs& a, int e4m3, int max_new, const bf16_t* q, bf16_t* out, const void* kc, const void* vc,
+                            void* workspace, hipStream_t s);
+
+}  // namespace caat

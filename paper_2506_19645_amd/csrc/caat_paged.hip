@@ -1,22 +1,9 @@
 // Paged key / value cache for gfx950: the new tokens of a ragged batch are rotated and stored to the pages of their sequences,
 // and attend to them.
 #include <math.h>
-#include "caat_internal.h"
+#include "caat_paged.h"
 
 namespace caat {
-
-static constexpr int PHD = 128;                  // head dim
-
-// Rows of sequence b: the first and how many; none unless they lie inside the packed rows.
-__device__ __forceinline__ int seq_rows(const PagedArgs& a, int b, int& first) {
-  if (!a.row_start) {
-    first = b;
-    return b < a.rows ? 1 : 0;
-  }
-  const int r0 = a.row_start[b], r1 = a.row_start[b + 1];
-  first = r0;
-  return r0 >= 0 && r1 > r0 && r1 <= a.rows ? r1 - r0 : 0;
-}
 
 // The sequence that owns a row (the first one, -1: none); called by whole waves, the answer is uniform.
 __device__ __forceinline__ int seq_of_row(const PagedArgs& a, int row, int& first, int& n) {
@@ -196,13 +183,12 @@ __global__ __launch_bounds__(256) void paged_attn_simple_kernel(const PagedArgs 
   *reinterpret_cast<unsigned*>(out + ((long long)rank * a.rows + row) * a.hpr * PHD + head * PHD + lane * 2) = pack2bf(o0 * inv, o1 * inv);
 }
 
-size_t paged_attn_workspace_bytes(int, int, int, long long) { return 0; }
+size_t paged_attn_workspace_bytes() { return paged_few_workspace_bytes(); }
 
 hipError_t launch_paged_attn(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, int max_new,
                              void* workspace, hipStream_t s) {
-  (void)max_new;
-  (void)workspace;
   if (a.rows == 0) return hipSuccess;
+  if ((long long)max_new * (a.hpr / a.kvpr) <= 64) return launch_paged_few(a, e4m3, max_new, q, out, kc, vc, workspace, s);
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)PHD);
   const dim3 grid((unsigned)a.rows, (unsigned)((a.T * a.hpr + 3) / 4));
   if (e4m3) hipLaunchKernelGGL(paged_attn_simple_kernel<true>, grid, dim3(256), 0, s, a, q, out, kc, vc, scale_log2);
