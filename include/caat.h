@@ -299,7 +299,7 @@ typedef struct caat_paged_desc {
   int head_dim;         /* 128 (CAAT_EUNSUPPORTED otherwise) */
   int cache_type;       /* caat_cache */
   int page_size;        /* positions per page, a multiple of 16 */
-  int max_pages;        /* columns of page_table */
+  int max_pages;        /* columns of page_table; max_pages * page_size at most 2^30 */
   long long n_pages;    /* pages of a rank's pool */
   long long rows;       /* token rows per rank of qkv, q and out */
   int max_new;          /* the most new tokens a sequence has in these calls: chooses the kernel, results do not depend on it

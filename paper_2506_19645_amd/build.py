@@ -14,7 +14,7 @@ SOURCES = ["caat_api.hip", "caat_gemm.hip", "caat_gemm_tiles_256x256.hip", "caat
            "caat_gemm_tiles_split.hip", "caat_gemm_pair_256x256.hip", "caat_gemm_pair_192x256.hip",
            "caat_gemm_pair_128x128.hip", "caat_gemm_pair_small.hip", "caat_gemm_stream.hip",
            "caat_stream.hip", "caat_attn.hip", "caat_decode_attn.hip",
-           "caat_paged.hip", "caat_paged_few.hip"]
+           "caat_paged.hip", "caat_paged_few.hip", "caat_paged_prompt.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-Wall", "-Wno-unused-function"]

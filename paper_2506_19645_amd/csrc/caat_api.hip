@@ -541,7 +541,7 @@ int paged_args(const caat_paged_desc* d, const int* row_start, const int* lens, 
   if (d->n_heads % d->T != 0 || d->n_heads % kv != 0 || kv % d->T != 0) return CAAT_ESHAPE;
   if (d->head_dim != 128) return CAAT_EUNSUPPORTED;
   constexpr long long MAX = 0x7FFFFFFFLL;
-  if (d->page_size % 16 != 0 || (long long)d->max_pages * d->page_size > MAX || d->n_pages > MAX) return CAAT_ESHAPE;
+  if (d->page_size % 16 != 0 || (long long)d->max_pages * d->page_size > (1LL << 30) || d->n_pages > MAX) return CAAT_ESHAPE;
   if (!row_start && d->batch > d->rows) return CAAT_ESHAPE;
   const long long hpr = d->n_heads / d->T, kvpr = kv / d->T;
   const long long hd = hpr * 128, qw = hd + 2 * kvpr * 128;
@@ -554,8 +554,7 @@ int paged_args(const caat_paged_desc* d, const int* row_start, const int* lens, 
   }
   if ((d->ld_q && (d->ld_q < hd || d->ld_q % 8 != 0)) || (d->ld_qkv && (d->ld_qkv < qw || d->ld_qkv % 8 != 0))) return CAAT_ESHAPE;
   // grids and row numbers are 32-bit
-  if (d->rows > MAX || d->rows * hpr > MAX || (long long)d->T * hpr > 65535 || hpr > 32768 || (long long)d->batch * d->T * hpr > MAX)
-    return CAAT_ESHAPE;
+  if (d->rows > MAX || d->rows * hpr > MAX || d->T * hpr > 65535 || (d->rows / 128 + d->batch + 1) * d->T * hpr > MAX) return CAAT_ESHAPE;
   a->row_start = row_start;
   a->lens = lens;
   a->table = page_table;

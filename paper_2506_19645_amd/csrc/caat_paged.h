@@ -26,9 +26,10 @@ __device__ __forceinline__ long long lane64(long long x, int lane) {   // a lane
                      (unsigned)__builtin_amdgcn_readlane((int)x, lane));
 }
 
-// The two forms of the attention.  `few`: a query tile is 16 (token, head of the group) rows, see caat_paged_few.hip
+// The two forms of the attention: caat_paged_few.hip, caat_paged_prompt.hip
 size_t paged_few_workspace_bytes();
 hipError_t launch_paged_few(const PagedArgs& a, int e4m3, int max_new, const bf16_t* q, bf16_t* out, const void* kc, const void* vc,
                             void* workspace, hipStream_t s);
+hipError_t launch_paged_prompt(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, hipStream_t s);
 
 }  // namespace caat

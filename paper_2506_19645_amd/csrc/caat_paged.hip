@@ -134,66 +134,12 @@ hipError_t launch_paged_append(const PagedArgs& a, int e4m3, const bf16_t* qkv, 
   return hipGetLastError();
 }
 
-// ---------------------------------------------------------------------------------------------------------
-// Attention, the simple form: a wave owns one (rank, row, query head) and walks the keys it sees, two channels per lane.
-template <bool E4M3>
-__device__ __forceinline__ float2 ld_pair(const void* base, long long at) {   // channels at, at + 1
-  if constexpr (E4M3) {
-    const unsigned w = *reinterpret_cast<const unsigned short*>((const unsigned char*)base + at);
-    const auto f = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
-    return make_float2(f[0], f[1]);
-  } else {
-    const unsigned w = *reinterpret_cast<const unsigned*>((const bf16_t*)base + at);
-    return make_float2(lo_bf(w), hi_bf(w));
-  }
-}
-template <bool E4M3>
-__global__ __launch_bounds__(256) void paged_attn_simple_kernel(const PagedArgs a, const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
-                                                                const void* __restrict__ kc, const void* __restrict__ vc, float scale_log2) {
-  const int lane = threadIdx.x & 63;
-  const int row = blockIdx.x, u = blockIdx.y * 4 + (threadIdx.x >> 6);
-  int first, n;
-  const int b = seq_of_row(a, row, first, n);
-  if (b < 0 || u >= a.T * a.hpr) return;
-  const int rank = u / a.hpr, head = u - rank * a.hpr, kvh = head / (a.hpr / a.kvpr);
-  const long long cap = (long long)a.max_pages * a.page_size;
-  const long long seen = min((long long)max(a.lens[b], 0) - n + (row - first) + 1, cap);
-  const unsigned qw = *reinterpret_cast<const unsigned*>(q + ((long long)rank * a.rows + row) * a.ld_q + head * PHD + lane * 2);
-  const float q0 = lo_bf(qw), q1 = hi_bf(qw);
-  if (a.k_scale) scale_log2 *= a.k_scale[rank * a.kvpr + kvh];
-  float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-  for (long long t = 0; t < seen; ++t) {
-    const long long col = t / a.page_size;
-    const int page = a.table[b * (long long)a.max_pages + col];
-    if (page < 0 || page >= a.n_pages) continue;
-    const long long at = rank * a.s_rank + page * a.s_page + kvh * a.s_head + (t - col * a.page_size) * a.s_row + lane * 2;
-    const float2 k = ld_pair<E4M3>(kc, at), v = ld_pair<E4M3>(vc, at);
-    float sc = q0 * k.x + q1 * k.y;
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) sc += __shfl_xor(sc, off, 64);
-    sc *= scale_log2;
-    const float m_new = fmaxf(m, sc), base = m_new == -INFINITY ? 0.0f : m_new;
-    const float alpha = exp2f(m - base), p = exp2f(sc - base);
-    l = l * alpha + p;
-    o0 = o0 * alpha + p * v.x;
-    o1 = o1 * alpha + p * v.y;
-    m = m_new;
-  }
-  const float inv = l == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[rank * a.kvpr + kvh] : 1.0f) / l;
-  *reinterpret_cast<unsigned*>(out + ((long long)rank * a.rows + row) * a.hpr * PHD + head * PHD + lane * 2) = pack2bf(o0 * inv, o1 * inv);
-}
-
 size_t paged_attn_workspace_bytes() { return paged_few_workspace_bytes(); }
 
 hipError_t launch_paged_attn(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, int max_new,
                              void* workspace, hipStream_t s) {
-  if (a.rows == 0) return hipSuccess;
   if ((long long)max_new * (a.hpr / a.kvpr) <= 64) return launch_paged_few(a, e4m3, max_new, q, out, kc, vc, workspace, s);
-  const float scale_log2 = 1.4426950408889634f / sqrtf((float)PHD);
-  const dim3 grid((unsigned)a.rows, (unsigned)((a.T * a.hpr + 3) / 4));
-  if (e4m3) hipLaunchKernelGGL(paged_attn_simple_kernel<true>, grid, dim3(256), 0, s, a, q, out, kc, vc, scale_log2);
-  else hipLaunchKernelGGL(paged_attn_simple_kernel<false>, grid, dim3(256), 0, s, a, q, out, kc, vc, scale_log2);
-  return hipGetLastError();
+  return launch_paged_prompt(a, e4m3, q, out, kc, vc, s);
 }
 
 }  // namespace caat

@@ -221,11 +221,10 @@ __global__ __launch_bounds__(64 * FNW) void paged_few_kernel(const PagedArgs a, 
         for (int dt = 0; dt < 8; ++dt) acc[dt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
       };
       start();
+      const bf16_t* src = q + (row_ok ? qrow * a.ld_q + head * PHD : 0);   // rows of nobody: any row, they see no key
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int dim = E4M3 ? 16 * g + 8 * (t & 1) + 64 * (t >> 1) : 32 * t + 8 * g;
-        qw[t] = row_ok ? *reinterpret_cast<const uint4*>(q + qrow * a.ld_q + head * PHD + dim) : make_uint4(0u, 0u, 0u, 0u);
-      }
+      for (int t = 0; t < 4; ++t)
+        qw[t] = *reinterpret_cast<const uint4*>(src + (E4M3 ? 16 * g + 8 * (t & 1) + 64 * (t >> 1) : 32 * t + 8 * g));
       bf16x8_t qf[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {

@@ -1,0 +1,439 @@
+// Attention of many new tokens per sequence (prompts and chunks of them) over a paged key / value cache, gfx950.
+//
+// What bounds it: the two products' MFMAs and the vector work per score beside them.  A workgroup of 4 waves owns 128 consecutive
+// (token, query head of the group) rows of one sequence, rank and key / value head, so grouped heads share the rows of K
+// and V; a wave owns 32 of them and walks the keys in blocks of 64 with an online softmax.  Scores are computed transposed
+// (S^T = K q^T, 32x32x16 MFMAs), so that a lane owns one query row and the exponentiated score registers, rounded to bf16, are the
+// k-slices of the second product; V comes through the LDS transpose read.  The body is software-pipelined inside a wave: the
+// score MFMAs of block b + 1 are issued one per step between the softmax arithmetic of block b.
+// K and V blocks (double buffered, chunk-swizzled) come from the pages directly, 16 keys of one page at a time; the table's
+// entries are read two blocks ahead of their use through the scalar cache.  An e4m3 block lands as it is in a buffer of
+// each wave's own and is widened to bf16 on its way into the tile, once per workgroup and not once per wave.
+#include <math.h>
+#include <algorithm>
+#include <type_traits>
+#include "caat_paged.h"
+
+namespace caat {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef short short8_t __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) const u32x4_t* lds_u4_t;
+typedef __attribute__((address_space(3))) const char* lds_c_t;
+typedef __attribute__((address_space(3))) short4_t* lds_s4_t;
+typedef __attribute__((address_space(4))) const int* const_i_t;
+
+static constexpr int PBQ = 128;                  // query rows per workgroup (32 per wave)
+static constexpr int PBK = 64;                   // keys per block
+static constexpr int PCH = PHD / 8;              // 16-byte chunks per row of a tile
+static constexpr int PTILE = PBK * PCH;          // chunks of a tile
+static constexpr int PRAW = 4 * 256;             // chunks of the waves' e4m3 buffers: 2 KB of K and 2 KB of V each
+
+__device__ __forceinline__ int pk_swz(int row, int c) { return c ^ (row & 15); }
+__device__ __forceinline__ int pv_swz(int row, int c) { return c ^ ((row & 3) << 2); }
+// the scores are MFMA results or -inf: a signalling input needs no quieting
+__device__ __forceinline__ float pmax3(float a, float b, float c) {
+  float d;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+  return d;
+}
+
+template <bool E4M3>
+__global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a, const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
+                                                              const void* __restrict__ kc, const void* __restrict__ vc, float scale_log2) {
+  constexpr int ELT = E4M3 ? 1 : 2;
+  __shared__ uint4 smem[4 * PTILE + (E4M3 ? PRAW : 0)];   // K slots 0 and 1, V slots 0 and 1, 16 KB each; e4m3 buffers
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = uni(tid >> 6);
+  const int frow = lane & 31, hf = lane >> 5;
+  const int grp = a.hpr / a.kvpr, heads = a.T * a.kvpr;
+
+  // ---- which rows: the launch runs through the tiles of all sequences, heads innermost (a head's tiles run on one XCD, close
+  // in time, where the number of heads is a multiple of 8), a sequence's last tile, which sees most keys, first
+  const int h = blockIdx.x % heads;
+  int tile = blockIdx.x / heads, b = -1, first = 0, n = 0;
+  for (int at = 0; at < a.batch && b < 0; at += 64) {
+    int f = 0, m = 0;
+    if (at + lane < a.batch) m = seq_rows(a, at + lane, f);
+    const int mine = (int)(((long long)m * grp + PBQ - 1) / PBQ);
+    int incl = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int up = __shfl_up(incl, off, 64);
+      if (lane >= off) incl += up;
+    }
+    const unsigned long long over = __ballot(incl > tile);
+    if (over) {
+      const int l = __builtin_ctzll(over);
+      tile -= __builtin_amdgcn_readlane(incl - mine, l);
+      first = __builtin_amdgcn_readlane(f, l);
+      n = __builtin_amdgcn_readlane(m, l);
+      tile = __builtin_amdgcn_readlane(mine, l) - 1 - tile;
+      b = at + l;
+    } else {
+      tile -= __builtin_amdgcn_readlane(incl, 63);
+    }
+  }
+  if (b < 0) return;                             // fewer tiles than the launch has room for
+  const int rank = h / a.kvpr, kvh = h - rank * a.kvpr;
+  const int len = max(uni(a.lens[b]), 0);
+  const int cap = a.max_pages * a.page_size;
+  const int keys = min(len, cap);
+  // keys that token t sees: below len - n + t + 1
+  const int row0 = tile * PBQ;
+  const int last_token = min(n - 1, (row0 + PBQ - 1) / grp);
+  const int kv_end = (int)min((long long)keys, (long long)len - n + last_token + 1);   // may be 0 or less
+  const int nblk = max(0, (kv_end + PBK - 1) / PBK);
+
+  // ---- Q fragments: B operand of S^T = K q^T: lane (row frow, k-half hf) holds q[16 ks + 8 hf .. + 7]
+  const int qr = row0 + wave * 32 + frow;
+  const int token = qr / grp, head = kvh * grp + (qr - token * grp);
+  const bool row_ok = token < n;
+  const long long qrow = (long long)rank * a.rows + first + token;
+  const int lim = row_ok ? (int)min((long long)len - n + token + 1, (long long)keys) : kv_end;
+  const int wave_lim = uni((int)min((long long)len - n + (row0 + wave * 32) / grp + 1, (long long)keys));   // of the wave's first row
+  bf16x8_t qf[PHD / 16];
+  {
+    uint4 w[PHD / 16];
+    const bf16_t* src = q + (row_ok ? qrow * a.ld_q + head * PHD : 0) + hf * 8;   // rows of nobody: any row, not stored
+#pragma unroll
+    for (int ks = 0; ks < PHD / 16; ++ks) w[ks] = *reinterpret_cast<const uint4*>(src + ks * 16);
+#pragma unroll
+    for (int ks = 0; ks < PHD / 16; ++ks) {
+      asm volatile("" : "+v"(w[ks].x), "+v"(w[ks].y), "+v"(w[ks].z), "+v"(w[ks].w));   // the wait for q stands in front of the loop
+      qf[ks] = __builtin_bit_cast(bf16x8_t, w[ks]);
+    }
+  }
+  if (E4M3 && a.k_scale) scale_log2 *= a.k_scale[h];
+
+  f32x16_t oacc[PHD / 32];
+#pragma unroll
+  for (int t = 0; t < PHD / 32; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[t][r] = 0.0f;
+  float m_run = -INFINITY, l_run = 0.0f;         // running maximum (raw score units) and this lane's share of the row sum
+
+  // ---- pages.  `next` holds the table's entries of the 4 groups of 16 keys of block (col, in) that is copied next; a block's
+  // places are made from them when its K is copied and kept for its V, one block later.
+  const const_i_t table = (const_i_t)(a.table + (long long)b * a.max_pages);
+  const int gpp = a.page_size >> 4;              // groups per page
+  int next[4], ncol = 0, nin = 0;                // entries, and column and group inside the page behind them
+  auto fetch = [&] {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      next[i] = table[min(ncol, a.max_pages - 1)];
+      if (++nin == gpp) {
+        nin = 0;
+        ++ncol;
+      }
+    }
+  };
+  struct Place {
+    long long at[4];                             // byte offsets of the groups inside a head's pages
+    unsigned have;                               // groups that have a page
+  };
+  int pin = 0;                                   // group inside its page of the block that is placed next
+  auto place = [&] {
+    Place p;
+    p.have = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool ok = next[i] >= 0 && next[i] < a.n_pages;
+      p.at[i] = ok ? (next[i] * a.s_page + (long long)pin * 16 * a.s_row) * ELT : 0;
+      p.have |= ok ? 1u << i : 0u;
+      if (++pin == gpp) pin = 0;
+    }
+    return p;
+  };
+  const unsigned char* kh = (const unsigned char*)kc + (rank * a.s_rank + kvh * a.s_head) * ELT;
+  const unsigned char* vh = (const unsigned char*)vc + (rank * a.s_rank + kvh * a.s_head) * ELT;
+
+  // ---- global -> LDS.  bf16: a copy fills 4 rows, the wave's rows 4 wave .. + 3 of each of the 4 groups.  e4m3: a copy fills 8 rows,
+  // a wave takes the group of its number, K and V.
+  const unsigned row_bytes = (unsigned)(a.s_row * ELT);
+  unsigned dko, dvo, dro = 0;
+  {
+    const int row = wave * 4 + (lane >> 4), phys = lane & 15;
+    dko = row * row_bytes + pk_swz(row, phys) * 16;       // (the swizzles repeat every 16 rows)
+    dvo = row * row_bytes + pv_swz(row, phys) * 16;
+    if (E4M3) dro = (lane >> 3) * row_bytes + (lane & 7) * 16;
+  }
+  auto issue_rows = [&](const unsigned char* base, unsigned off, const Place& p, int blk, uint4* t) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int left = p.have >> i & 1 ? kv_end - blk * PBK - i * 16 : 0;   // rows of the group that anybody sees
+      const i32x4_t rs = make_rsrc(base + p.at[i]);
+      dma16(rs, wave * 4 + (lane >> 4) < left ? off : 0x80000000u, t + (i * 16 + wave * 4) * PCH);
+    }
+  };
+  uint4* raw = smem + 4 * PTILE + (E4M3 ? wave * 256 : 0);
+  auto issue_raw = [&](const unsigned char* base, const Place& p, int blk, uint4* t) {   // the wave's group
+    const int left = p.have >> wave & 1 ? kv_end - blk * PBK - wave * 16 : 0;
+    const long long at = wave == 0 ? p.at[0] : wave == 1 ? p.at[1] : wave == 2 ? p.at[2] : p.at[3];
+    const i32x4_t rs = make_rsrc(base + at);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      dma16(rs, i * 8 + (lane >> 3) < left ? dro + i * 8 * row_bytes : 0x80000000u, t + i * 64);
+  };
+  // the wave's group of a raw block as bf16 rows of the tile: lane = row (lane / 4) and a quarter of it
+  auto widen = [&](const uint4* src, uint4* tile_at, bool is_v) {
+    const int r = lane >> 2, part = lane & 3, row = wave * 16 + r;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const uint4 w = src[r * 8 + part * 2 + c];
+      const unsigned x[4] = {w.x, w.y, w.z, w.w};
+      unsigned y[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        y[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x[i], 1.0f, false));
+        y[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x[i], 1.0f, true));
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int ch = part * 4 + c * 2 + i;
+        tile_at[row * PCH + (is_v ? pv_swz(row, ch) : pk_swz(row, ch))] = make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+      }
+    }
+  };
+  auto kslot = [&](int blk) { return smem + (blk & 1) * PTILE; };
+  auto vslot = [&](int blk) { return smem + (2 + (blk & 1)) * PTILE; };
+
+  // Per-lane LDS addresses of the fragment reads; slot, key tile and 16-key slice go into the instructions' immediate offsets.
+  //   K fragment (32 rows x one chunk): row = 32 j + frow, logical chunk 2 ks + hf
+  //   V transpose read: row = 16 u + 4 hf + (i16 >> 2) (+ 8), column 32 dt + 16 half + 4 (i16 & 3)
+  constexpr int TILE_BYTES = PTILE * 16;
+  lds_u4_t koff[PHD / 16];
+  lds_c_t voff[PHD / 32];
+  {
+    const lds_c_t lds0 = (lds_c_t)smem;
+#pragma unroll
+    for (int ks = 0; ks < PHD / 16; ++ks) koff[ks] = (lds_u4_t)(lds0 + (frow * PCH + pk_swz(frow, ks * 2 + hf)) * 16);
+    const int i16 = lane & 15, half = (lane >> 4) & 1;
+    const int vrow = 4 * hf + (i16 >> 2);
+#pragma unroll
+    for (int dt = 0; dt < PHD / 32; ++dt) {
+      const int col = dt * 32 + half * 16 + (i16 & 3) * 4;
+      voff[dt] = lds0 + ((vrow * PCH + pv_swz(vrow, col >> 3)) * 16 + (col & 7) * 2);
+    }
+  }
+  const f32x16_t zero16 = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+  const bf16x2_t ones2 = {(__bf16)1.0f, (__bf16)1.0f};
+
+  Place pk, pv;                                  // of the block whose K was copied last, of the one whose V is next
+  unsigned have = 0, have_next = 0;              // groups with a page of the block in the softmax, of the one behind it
+
+  // One key block: the scores of block blk are in `scur`; those of blk + 1 are made into `snext` under its softmax
+  auto key_block = [&](int blk, f32x16_t* scur, f32x16_t* snext, auto slot_c, auto last_c) {
+    constexpr int SLOT = decltype(slot_c)::value;
+    constexpr bool LAST = decltype(last_c)::value;
+    wait_vmcnt<0>();
+    __syncthreads();                             // K(blk + 1) and V(blk) are there; everyone is done with K(blk) and V(blk - 1)
+    if constexpr (E4M3) {
+      // K(blk + 2) and V(blk + 1) lie in the wave's buffer, K(blk + 3) and V(blk + 2) take their place
+      if (blk + 2 < nblk) widen(raw, kslot(blk), false);
+      if (blk + 1 < nblk) widen(raw + 128, vslot(blk + 1), true);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      pv = pk;
+      if (blk + 3 < nblk) {
+        pk = place();
+        fetch();
+        issue_raw(kh, pk, blk + 3, raw);
+      }
+      if (blk + 2 < nblk) issue_raw(vh, pv, blk + 2, raw + 128);
+    } else {
+      pv = pk;
+      if (blk + 2 < nblk) {
+        pk = place();
+        fetch();
+        issue_rows(kh, dko, pk, blk + 2, kslot(blk));
+      }
+      if (blk + 1 < nblk) issue_rows(vh, dvo, pv, blk + 1, vslot(blk + 1));
+    }
+    const int kv0 = blk * PBK;
+    // ---- mask (keys of register r: kv0 + 32 j + 8 (r / 4) + 4 hf + r % 4): only where some row of the wave does not see the whole
+    // block, or a group has no page
+    if (kv0 + PBK > wave_lim || have != 15u) {
+#pragma unroll
+      for (int j = 0; j < PBK / 32; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = kv0 + j * 32 + 8 * (r >> 2) + 4 * hf + (r & 3);
+          if (key >= lim || !(have >> (j * 2 + (r >> 3)) & 1)) scur[j][r] = -INFINITY;
+        }
+    }
+    have = have_next;
+    have_next = E4M3 ? pv.have : pk.have;
+    // ---- one MFMA per step, a scheduling fence behind each:
+    //   steps 0-15 : score MFMAs of block blk + 1 (fragments read three steps ahead); underneath: the row maximum (steps 0-3),
+    //                its exchange with the other half-row (4-5), the exponentials of keys 0-31 (6-13)
+    //   steps 16-31: second-product MFMAs; underneath: the exponentials of keys 32-63 (steps 16-23)
+    auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+    auto kread = [&](int idx) -> u32x4_t { return koff[idx & 7][((SLOT ^ 1) * TILE_BYTES + (idx >> 3) * 32 * PCH * 16) / 16]; };
+    float mx = -INFINITY, mxo = 0.0f, m_new = 0.0f, alpha = 1.0f, mb = 0.0f, psum = 0.0f;
+    unsigned pw[PBK / 2];                        // the block's probabilities, bf16 pairs
+    auto prob_pair = [&](int i) {
+      const int j = i >> 3, r = (i & 7) * 2;
+      const float p0 = __builtin_amdgcn_exp2f(scur[j][r] * scale_log2 - mb);
+      const float p1 = __builtin_amdgcn_exp2f(scur[j][r + 1] * scale_log2 - mb);
+      pw[i] = pack2bf(p0, p1);
+      // the row sum takes the probabilities as the second product sees them, two per instruction
+      psum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pw[i]), ones2, psum, false);
+      asm volatile("" : "+v"(pw[i]), "+v"(psum));   // pins the pair to this place in the stream
+    };
+    u32x4_t kr[3];
+    if constexpr (!LAST) {
+      kr[0] = kread(0);
+      kr[1] = kread(1);
+      kr[2] = kread(2);
+    }
+    fence();
+#pragma unroll
+    for (int idx = 0; idx < 16; ++idx) {
+      if constexpr (!LAST) {
+        const int j = idx >> 3, ks = idx & 7;
+        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, kr[idx % 3]);
+        snext[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], ks == 0 ? zero16 : snext[j], 0, 0, 0);
+        if (idx + 3 < 16) kr[idx % 3] = kread(idx + 3);
+      }
+      if (idx < 4) {
+        const int j = idx >> 1, r0 = (idx & 1) * 8;
+#pragma unroll
+        for (int r = 0; r < 8; r += 2) mx = pmax3(mx, scur[j][r0 + r], scur[j][r0 + r + 1]);
+        if (idx == 3) mxo = __shfl_xor(mx, 32, 64);
+      } else if (idx == 5) {
+        m_new = fmaxf(m_run, fmaxf(mx, mxo));
+        const float mz = m_new == -INFINITY ? 0.0f : m_new;   // no key seen so far: nothing is added
+        alpha = __builtin_amdgcn_exp2f((m_run - mz) * scale_log2);
+        mb = mz * scale_log2;
+      } else if (idx >= 6 && idx < 14) {
+        prob_pair(idx - 6);
+      }
+      fence();
+    }
+    if (__any(m_new != m_run)) {                 // the running maximum settles after the first blocks
+#pragma unroll
+      for (int t = 0; t < PHD / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[t][r] *= alpha;
+    }
+    m_run = m_new;
+
+    // ---- O^T += V^T P^T: k-slice u (16 keys): lane half hf contributes keys 16 u + 4 hf + {0 .. 3} and 16 u + 8 + 4 hf + {0 .. 3}
+    auto vread = [&](int st, short4_t& v0, short4_t& v1) {
+      const lds_c_t a0 = voff[st & 3] + ((2 + SLOT) * TILE_BYTES + (st >> 2) * 16 * PCH * 16);
+      v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t)a0);
+      v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t)(a0 + 8 * PCH * 16));
+    };
+    short4_t va[3], vb[3];
+    vread(0, va[0], vb[0]);
+    vread(1, va[1], vb[1]);
+    vread(2, va[2], vb[2]);
+    fence();
+#pragma unroll
+    for (int st = 0; st < 16; ++st) {
+      const int u = st >> 2, dt = st & 3;
+      const short8_t vv = {va[st % 3][0], va[st % 3][1], va[st % 3][2], va[st % 3][3],
+                           vb[st % 3][0], vb[st % 3][1], vb[st % 3][2], vb[st % 3][3]};
+      const bf16x8_t pfu = __builtin_bit_cast(bf16x8_t, make_uint4(pw[4 * u], pw[4 * u + 1], pw[4 * u + 2], pw[4 * u + 3]));
+      oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vv), pfu, oacc[dt], 0, 0, 0);
+      if (st + 3 < 16) vread(st + 3, va[st % 3], vb[st % 3]);
+      if (st < 8) prob_pair(8 + st);
+      fence();
+    }
+    l_run = l_run * alpha + psum;
+  };
+
+  if (nblk > 0) {
+    // prologue: K(0) alone first (its scores open the pipeline), then what the first loop iteration expects
+    f32x16_t sa[PBK / 32], sb[PBK / 32];
+    fetch();
+    pk = place();
+    fetch();
+    if constexpr (E4M3) {
+      issue_raw(kh, pk, 0, raw);
+      issue_raw(vh, pk, 0, raw + 128);
+      const unsigned have0 = pk.have;
+      wait_vmcnt<0>();
+      widen(raw, kslot(0), false);
+      widen(raw + 128, vslot(0), true);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      have = have0;
+      if (1 < nblk) {
+        pk = place();
+        fetch();
+        issue_raw(kh, pk, 1, raw);
+        issue_raw(vh, pk, 1, raw + 128);
+        wait_vmcnt<0>();
+        widen(raw, kslot(1), false);             // V(1) stays in the buffer for the first iteration
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        have_next = pk.have;
+        if (2 < nblk) {
+          pk = place();
+          fetch();
+          issue_raw(kh, pk, 2, raw);
+        }
+      }
+      __syncthreads();
+    } else {
+      issue_rows(kh, dko, pk, 0, kslot(0));
+      wait_vmcnt<0>();
+      __syncthreads();
+      have = pk.have;
+      issue_rows(vh, dvo, pk, 0, vslot(0));
+      if (1 < nblk) {
+        pk = place();
+        fetch();
+        issue_rows(kh, dko, pk, 1, kslot(1));
+      }
+      have_next = pk.have;
+    }
+#pragma unroll
+    for (int j = 0; j < PBK / 32; ++j)
+#pragma unroll
+      for (int ks = 0; ks < PHD / 16; ++ks) {
+        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, koff[ks][(j * 32 * PCH * 16) / 16]);
+        sa[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], ks == 0 ? zero16 : sa[j], 0, 0, 0);
+      }
+    int blk = 0;
+    for (; blk + 2 < nblk; blk += 2) {
+      key_block(blk, sa, sb, std::integral_constant<int, 0>{}, std::false_type{});
+      key_block(blk + 1, sb, sa, std::integral_constant<int, 1>{}, std::false_type{});
+    }
+    if (blk + 1 < nblk) {
+      key_block(blk, sa, sb, std::integral_constant<int, 0>{}, std::false_type{});
+      key_block(blk + 1, sb, sa, std::integral_constant<int, 1>{}, std::true_type{});
+    } else {
+      key_block(blk, sa, sb, std::integral_constant<int, 0>{}, std::true_type{});
+    }
+  }
+
+  // ---- normalise and store: lane holds out[row][32 dt + 8 (r / 4) + 4 hf + r % 4]
+  l_run += __shfl_xor(l_run, 32, 64);
+  if (row_ok) {
+    const float inv = l_run == 0.0f ? 0.0f : (E4M3 && a.v_scale ? a.v_scale[h] : 1.0f) / l_run;
+    bf16_t* o = out + (qrow * a.hpr + head) * PHD;
+#pragma unroll
+    for (int dt = 0; dt < PHD / 32; ++dt)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint2 w;
+        w.x = pack2bf(oacc[dt][k * 4 + 0] * inv, oacc[dt][k * 4 + 1] * inv);
+        w.y = pack2bf(oacc[dt][k * 4 + 2] * inv, oacc[dt][k * 4 + 3] * inv);
+        *reinterpret_cast<uint2*>(o + dt * 32 + k * 8 + hf * 4) = w;
+      }
+  }
+}
+
+hipError_t launch_paged_prompt(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, hipStream_t s) {
+  const long long grp = a.hpr / a.kvpr;
+  const long long tiles = std::min<long long>(a.rows * grp / PBQ + a.batch, a.rows * grp);   // at most: one per sequence is not full
+  const float scale_log2 = 1.4426950408889634f / sqrtf((float)PHD);
+  auto kernel = e4m3 ? paged_prompt_kernel<true> : paged_prompt_kernel<false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles * a.T * a.kvpr)), dim3(256), 0, s, a, q, out, kc, vc, scale_log2);
+  return hipGetLastError();
+}
+
+}  // namespace caat
