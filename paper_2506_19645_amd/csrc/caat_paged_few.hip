@@ -1,7 +1,7 @@
 // Attention of few new tokens per sequence (decode steps, drafted tokens) over a paged key / value cache, gfx950.
 //
-// What bounds it: the K / V rows, read once from HBM.  The unit of work is a tile of 16 (token, query head of the group) rows of
-// one sequence, rank and key / value head, times a block of keys (16 in bf16, 32 in e4m3: 8 KB of K and V).  The blocks of
+// What bounds it: the K / V rows, read once from HBM.  The unit of work is up to three tiles of 16 (token, query head of the group)
+// rows of one sequence, rank and key / value head, times a block of keys (16 in bf16, 32 in e4m3: 8 KB of K and V).  The blocks of
 // all units stand in one line, sequence by sequence, and every WAVE of the launch takes an equal stretch of it, so a batch of
 // one long and many short sequences fills the chip like an even one, whatever the lengths (which only the device
 // knows).  A wave copies its blocks global -> LDS into two slots that only it reads, waits for its own copies alone, and computes
@@ -29,14 +29,13 @@ static constexpr int FNS = 2;
 static constexpr int FNI = 8;                    // 1 KB copies per block: 4 of K, 4 of V
 static constexpr int FPR = PHD + 4;              // floats of a partial row: 128 sums, maximum, denominator, 2 unused
 static constexpr int FMAX_WGS = 512;             // workgroups of a launch
-static constexpr long long FSLOT = 16 * FPR;     // floats of a partial result
 
-// What the wave in which a unit begins says about it, if it ends in another one.
+// What the wave in which a unit begins says about it.  They stand in the order of the units where the launch cannot have more
+// units than waves, in that of the waves (of which one begins at most one unit that it does not finish) otherwise.
 struct FewJoin {
-  int rows;                                      // 0: nothing to join
-  int rank, kvh, first, tile;
-  int unused;
-  long long begin, end, per;                     // blocks of the unit in the line of all blocks; length of a stretch
+  int rows;                                      // 0: the unit was finished by that wave
+  int rank, kvh, first, row0;                    // row0: the unit's first (token, head) row of the sequence
+  int begin, end, per;                           // the unit's blocks in the line of all of them; length of a stretch
 };
 
 // Swizzles of the 16-byte chunks of a row in LDS (256-byte rows in bf16, 128 in e4m3): K is read 16 rows x one chunk at a
@@ -54,19 +53,40 @@ __device__ __forceinline__ unsigned fp8_hi(unsigned w) {
 // A chunk of 64 sequences in registers: lane l holds sequence at + l
 struct SeqChunk {
   int at, first, n, len;
-  long long work;                                // blocks of one (rank, key / value head)
+  int units, work;                               // of one (rank, key / value head): units and their length in the line
 };
 
-template <bool E4M3>
-__global__ __launch_bounds__(64 * FNW) void paged_few_kernel(const PagedArgs a, const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
+// inclusive sums over the lanes of a wave
+__device__ __forceinline__ int wave_sums(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // from 1, 2, 4, 8 lanes below inside rows of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // the last lane of rows 0 and 2 to rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // lane 31 to rows 2 and 3
+  return v;
+}
+
+// How the units are dealt out.  FEW_LINE: as the head of this file says.  FEW_WAVE: whole units to waves, FEW_WG: a unit to a
+// workgroup, a quarter of its blocks to each wave; neither leaves anything for the second kernel.
+enum FewMode { FEW_LINE = 0, FEW_WAVE = 1, FEW_WG = 2 };
+// A unit's start (its queries' and pages' way, the first block's, its results) takes about as long as this many blocks: it
+// stands in the line in front of them.
+static constexpr int FSTART = 3;
+
+// NT: tiles of 16 query rows of a unit, which share the fragments of K and V
+template <bool E4M3, int NT>
+__global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs a, const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
                                                              const void* __restrict__ kc, const void* __restrict__ vc,
                                                              float* __restrict__ part, FewJoin* __restrict__ joins, float scale_log2,
-                                                             int least, int whole) {
+                                                             int least, int mode, int unit_joins) {
   constexpr int KB = E4M3 ? 32 : 16;             // keys per block
   constexpr int HV = KB / 16;                    // groups of 16 keys, each inside one page
   constexpr int ELT = E4M3 ? 1 : 2;
   constexpr int RPC = 1024 / (PHD * ELT);        // rows per copy: 4 or 8
   constexpr int CPR = 64 / RPC;                  // 16-byte chunks per row
+  constexpr int ROWS = 16 * NT;                  // query rows of a unit
+  constexpr long long FSLOT = ROWS * FPR;        // floats of a partial result
   __shared__ uint4 ring[FNW * FNS * FNI * 64];
   static_assert(FNW * 16 * FPR * 4 <= FNW * FNS * FNI * 1024, "the partial results take the rings' place");
   __shared__ float s_m[FNW][16], s_l[FNW][16];
@@ -75,73 +95,86 @@ __global__ __launch_bounds__(64 * FNW) void paged_few_kernel(const PagedArgs a, 
   const int r16 = lane & 15, g = lane >> 4;
   const int grp = a.hpr / a.kvpr, heads = a.T * a.kvpr;
   const int wid = blockIdx.x * FNW + wave;
-  const long long cap = (long long)a.max_pages * a.page_size;
+  const int cap = a.max_pages * a.page_size;
 
   // ---- the line of all blocks, and this wave's stretch of it
   auto load_seqs = [&](int at) {
     SeqChunk c;
     c.at = at;
-    c.first = c.n = c.len = 0;
+    c.first = c.n = c.len = c.units = 0;
     c.work = 0;
     if (at + lane < a.batch) {
       c.n = seq_rows(a, at + lane, c.first);
       c.len = max(a.lens[at + lane], 0);
-      const long long keys = min((long long)c.len, cap);
-      const long long nb = whole ? 1 : max((keys + KB - 1) / KB, 1LL);
-      c.work = ((long long)c.n * grp + 15) / 16 * nb;
+      const int nb = mode == FEW_LINE ? (min(c.len, cap) + KB - 1) / KB + FSTART : 1;
+      c.units = (int)(((long long)c.n * grp + ROWS - 1) / ROWS);
+      c.work = c.units * nb;
     }
     return c;
   };
   SeqChunk sq = load_seqs(0);
-  long long total = sq.work;
-  for (int at = 64; at < a.batch; at += 64) total += load_seqs(at).work;
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
-  total = uni64(total) * heads;
+  int work_to = wave_sums(sq.work), units_to = wave_sums(sq.units);
+  int total = __builtin_amdgcn_readlane(work_to, 63), units = __builtin_amdgcn_readlane(units_to, 63);
+  for (int at = 64; at < a.batch; at += 64) {
+    const SeqChunk c = load_seqs(at);
+    total += __builtin_amdgcn_readlane(wave_sums(c.work), 63);
+    units += __builtin_amdgcn_readlane(wave_sums(c.units), 63);
+  }
+  total *= heads;                                // (the host has checked that this is below 2^31)
+  units *= heads;
   const int nwaves = gridDim.x * FNW;
-  const long long per = max((total + nwaves - 1) / nwaves, (long long)least);
-  const long long x0 = wid * per, x1 = min(x0 + per, total);
+  const int per = mode == FEW_WG ? 1 : max((int)((unsigned)(total + nwaves - 1) / (unsigned)nwaves), least);
+  const int x0 = (int)min((long long)(mode == FEW_WG ? blockIdx.x : wid) * per, (long long)total), x1 = min(total - x0, per) + x0;
   FewJoin join = {};
   if (x0 < x1) {
-    // the sequence of block x0: `base` is the place of its first block
-    int b = 0;
-    long long base = 0;
-    for (;;) {
-      long long incl = sq.work;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const long long up = __shfl_up(incl, off, 64);
-        if (lane >= off) incl += up;
-      }
-      const unsigned long long over = __ballot(base + incl * heads > x0);
+    // the sequence of place x0: `base` is where its first unit begins, unit0 the number of that unit.  (There is one, unless the
+    // list of rows gives some twice and the line is longer than 31 bits: then this wave does nothing.)
+    int b = a.batch, unit0 = 0, base = 0;
+    while (sq.at < a.batch) {
+      const unsigned long long over = __ballot(base + work_to * heads > x0);
       if (over) {
         b = __builtin_ctzll(over);
-        base += lane64(incl - sq.work, b) * heads;
+        base += __builtin_amdgcn_readlane(work_to - sq.work, b) * heads;
+        unit0 += __builtin_amdgcn_readlane(units_to - sq.units, b) * heads;
         b += sq.at;
         break;
       }
-      base += lane64(incl, 63) * heads;          // (some chunk holds x0 < total)
+      base += __builtin_amdgcn_readlane(work_to, 63) * heads;
+      unit0 += __builtin_amdgcn_readlane(units_to, 63) * heads;
       sq = load_seqs(sq.at + 64);
+      work_to = wave_sums(sq.work);
+      units_to = wave_sums(sq.units);
     }
     int pages = -1, page0 = -1, pages_of = -1;   // lane l: entry page0 + l of sequence pages_of's table, -1: no page
     uint4* mine = ring + wave * (FNS * FNI * 64);
 
-    for (long long x = x0; x < x1;) {
+    for (int x = x0; x < x1 && b < a.batch;) {
       const int sl = b - sq.at;
       const int n = __builtin_amdgcn_readlane(sq.n, sl), first = __builtin_amdgcn_readlane(sq.first, sl);
-      const int len = __builtin_amdgcn_readlane(sq.len, sl);
-      const long long work = lane64(sq.work, sl);
-      const int keys = (int)min((long long)len, cap);
+      const int len = __builtin_amdgcn_readlane(sq.len, sl), work = __builtin_amdgcn_readlane(sq.work, sl);
+      const int tiles = __builtin_amdgcn_readlane(sq.units, sl);
+      const int keys = min(len, cap);
       const int nblk = (keys + KB - 1) / KB;     // may be 0
-      const int nb = whole ? 1 : max(nblk, 1);
-      const int tiles = (n * grp + 15) >> 4;
-      const long long o = x - base;
-      const long long u = (o >> 32) ? o / nb : (long long)((unsigned)o / (unsigned)nb);
-      const int from = (int)(o - u * nb);
-      const int to = (int)min((long long)nb, from + (x1 - x));
-      const int h = (int)(u / tiles), tile = (int)(u - (long long)h * tiles);
+      const int nb = mode == FEW_LINE ? nblk + FSTART : 1;
+      const int u = (int)((unsigned)(x - base) / (unsigned)nb);
+      const int unit = base + u * nb;            // place of the unit
+      const int to = min(unit + nb, x1);         // and of the stretch's part of it: x .. to - 1
+      const int h = (int)((unsigned)u / (unsigned)tiles), tile = u - h * tiles;
       const int rank = h / a.kvpr, kvh = h - rank * a.kvpr;
-      const int k0 = whole ? 0 : from, k1 = whole ? nblk : min(to, nblk);   // blocks of keys
+      // its blocks of keys
+      int k0, k1;
+      if (mode == FEW_LINE) {
+        k0 = max(x - unit - FSTART, 0);
+        k1 = max(to - unit - FSTART, 0);
+        if (to < unit + nb && k1 == 0) break;    // the stretch ends in front of the first one
+      } else if (mode == FEW_WAVE) {
+        k0 = 0;
+        k1 = nblk;
+      } else {
+        k0 = nblk * wave / FNW;
+        k1 = nblk * (wave + 1) / FNW;
+      }
+      const bool begins = unit + FSTART >= x0;   // FEW_LINE: its first block lies in this stretch
 
       // ---- pages: the table's entries from the first one on
       auto take_pages = [&](int col) {
@@ -198,39 +231,49 @@ __global__ __launch_bounds__(64 * FNW) void paged_few_kernel(const PagedArgs a, 
         return have;
       };
 
-      // ---- query rows: lane r16 owns row tile * 16 + r16 = (token, head of the group)
-      const int qr = tile * 16 + r16;
-      const int token = qr / grp, head = kvh * grp + (qr - token * grp);
-      const bool row_ok = token < n;
-      const long long qrow = (long long)rank * a.rows + first + token;
-      // keys below lim are seen; the arithmetic cannot overflow: len >= 0, token < n <= 2^31
-      const int lim = row_ok ? (int)min((long long)len - n + token + 1, (long long)keys) : 0;
-      uint4 qw[4];
+      // ---- query rows: lane r16 owns rows tile * ROWS + 16 nt + r16 = (token, head of the group)
+      bool row_ok[NT];
+      int lim[NT];                               // keys below are seen
+      long long qat[NT];                         // (rank's row) * heads + head
+      bf16x8_t qf[NT][4];
       unsigned have[FNS];
-      float m, l;
-      f32x4_t acc[8];
+      float m[NT], l[NT];
+      f32x4_t acc[NT][8];
       auto start = [&] {
         col = k0 * KB / a.page_size;
         inpage = k0 * KB - col * a.page_size;
         if (col < page0) take_pages(col);
 #pragma unroll
         for (int i = 0; i < FNS; ++i) have[i] = copy(k0 + i, i);
-        m = -INFINITY;
-        l = 0.0f;
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) acc[dt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int nt = 0; nt < NT; ++nt) {
+          m[nt] = -INFINITY;
+          l[nt] = 0.0f;
+#pragma unroll
+          for (int dt = 0; dt < 8; ++dt) acc[nt][dt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        }
       };
       start();
-      const bf16_t* src = q + (row_ok ? qrow * a.ld_q + head * PHD : 0);   // rows of nobody: any row, they see no key
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-        qw[t] = *reinterpret_cast<const uint4*>(src + (E4M3 ? 16 * g + 8 * (t & 1) + 64 * (t >> 1) : 32 * t + 8 * g));
-      bf16x8_t qf[4];
+      for (int nt = 0; nt < NT; ++nt) {
+        const int qr = tile * ROWS + nt * 16 + r16;
+        const int token = qr / grp, head = kvh * grp + (qr - token * grp);
+        const long long qrow = (long long)rank * a.rows + first + token;
+        row_ok[nt] = token < n;
+        lim[nt] = row_ok[nt] ? min(len - n + token + 1, keys) : 0;   // (len >= 0 and token < n: no overflow)
+        qat[nt] = qrow * a.hpr + head;
+        const bf16_t* src = q + (row_ok[nt] ? qrow * a.ld_q + head * PHD : 0);   // rows of nobody: any row, they see no key
+        uint4 qw[4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        asm volatile("" : "+v"(qw[t].x), "+v"(qw[t].y), "+v"(qw[t].z), "+v"(qw[t].w));   // the wait for q stands in front of the loop
-        qf[t] = __builtin_bit_cast(bf16x8_t, qw[t]);
+        for (int t = 0; t < 4; ++t)
+          qw[t] = *reinterpret_cast<const uint4*>(src + (E4M3 ? 16 * g + 8 * (t & 1) + 64 * (t >> 1) : 32 * t + 8 * g));
+#pragma unroll
+        for (int t = 0; t < 4; ++t) qf[nt][t] = __builtin_bit_cast(bf16x8_t, qw[t]);
       }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) asm volatile("" : "+v"(qf[nt][t]));   // the wait for q stands in front of the loop
       const float sc_log2 = E4M3 && a.k_scale ? scale_log2 * a.k_scale[h] : scale_log2;
 
       auto sweep = [&](auto fp32_c) {            // the first FNS copies are under way
@@ -273,95 +316,106 @@ __global__ __launch_bounds__(64 * FNW) void paged_few_kernel(const PagedArgs a, 
           have[0] = have[1];
           have[1] = copy(blk + FNS, slot);
           slot ^= 1;
-          f32x4_t sc[HV];
+          uint4 kf[HV][4];                       // dims of step t, for all query tiles
 #pragma unroll
-          for (int j = 0; j < HV; ++j) {
-            sc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+          for (int j = 0; j < HV; ++j)
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-              uint4 kf;
               if constexpr (E4M3) {
                 const uint4 w = kw[j * 2 + (t >> 1)];
                 const unsigned w0 = t & 1 ? w.z : w.x, w1 = t & 1 ? w.w : w.y;
-                kf = make_uint4(fp8_lo(w0), fp8_hi(w0), fp8_lo(w1), fp8_hi(w1));
+                kf[j][t] = make_uint4(fp8_lo(w0), fp8_hi(w0), fp8_lo(w1), fp8_hi(w1));
               } else {
-                kf = kw[t];
+                kf[j][t] = kw[t];
               }
-              sc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf), qf[t], sc[j], 0, 0, 0);
             }
-          }
-          // scores of query row r16 and keys blk * KB + 16 j + 4 g + i
-          float p[HV][4], mx = -INFINITY;
+          // scores of query row r16 of tile nt and keys blk * KB + 16 j + 4 g + i, then their probabilities in two parts
+          unsigned hi[NT][HV][2], lo[NT][HV][2];
 #pragma unroll
-          for (int j = 0; j < HV; ++j)
+          for (int nt = 0; nt < NT; ++nt) {
+            f32x4_t sc[HV];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int key = blk * KB + 16 * j + 4 * g + i;
-              p[j][i] = key < lim && (pg >> j & 1) ? sc[j][i] * sc_log2 : -INFINITY;
-              mx = fmaxf(mx, p[j][i]);
+            for (int j = 0; j < HV; ++j) {
+              sc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+              for (int t = 0; t < 4; ++t)
+                sc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[j][t]), qf[nt][t], sc[j], 0, 0, 0);
             }
-          mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-          const float m_new = fmaxf(m, mx);
-          const float mb = m_new == -INFINITY ? 0.0f : m_new;   // no key seen so far: nothing is added
-          const float alpha = __builtin_amdgcn_exp2f(m - mb);
-          float sum = 0.0f;
+            float p[HV][4], mx = -INFINITY;
 #pragma unroll
-          for (int j = 0; j < HV; ++j)
+            for (int j = 0; j < HV; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              p[j][i] = __builtin_amdgcn_exp2f(p[j][i] - mb);
-              sum += p[j][i];
-            }
-          l = l * alpha + sum;
-          m = m_new;
-#pragma unroll
-          for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[dt][r] *= alpha;
-          if constexpr (decltype(fp32_c)::value) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)          // step i of the product: the keys 4 g + i, g = 0 .. 3 (bf16 caches only)
-#pragma unroll
-              for (int dt = 0; dt < 8; ++dt) {
-                const unsigned w = i & 2 ? vw[dt].y : vw[dt].x;
-                acc[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(i & 1 ? hi_bf(w) : lo_bf(w), p[0][i], acc[dt], 0, 0, 0);
+              for (int i = 0; i < 4; ++i) {
+                const int key = blk * KB + 16 * j + 4 * g + i;
+                p[j][i] = key < lim[nt] && (pg >> j & 1) ? sc[j][i] * sc_log2 : -INFINITY;
+                mx = fmaxf(mx, p[j][i]);
               }
-          } else {
-            unsigned hi[HV][2], lo[HV][2];
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float m_new = fmaxf(m[nt], mx);
+            const float mb = m_new == -INFINITY ? 0.0f : m_new;   // no key seen so far: nothing is added
+            if (__any(m_new != m[nt])) {         // the running maximum settles after the first blocks
+              const float alpha = __builtin_amdgcn_exp2f(m[nt] - mb);
+              l[nt] *= alpha;
+#pragma unroll
+              for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[nt][dt][r] *= alpha;
+              m[nt] = m_new;
+            }
+#pragma unroll
+            for (int j = 0; j < HV; ++j)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                p[j][i] = __builtin_amdgcn_exp2f(p[j][i] - mb);
+                l[nt] += p[j][i];
+              }
 #pragma unroll
             for (int j = 0; j < HV; ++j)
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
-                hi[j][i] = pack2bf(p[j][2 * i], p[j][2 * i + 1]);
-                lo[j][i] = pack2bf(p[j][2 * i] - lo_bf(hi[j][i]), p[j][2 * i + 1] - hi_bf(hi[j][i]));
+                const float p0 = p[j][2 * i], p1 = p[j][2 * i + 1];
+                hi[nt][j][i] = pack2bf(p0, p1);
+                lo[nt][j][i] = pack2bf(p0 - lo_bf(hi[nt][j][i]), p1 - hi_bf(hi[nt][j][i]));
               }
-            if constexpr (E4M3) {                // the 32 keys' first parts, then their second
-              const bf16x8_t ph = __builtin_bit_cast(bf16x8_t, make_uint4(hi[0][0], hi[0][1], hi[1][0], hi[1][1]));
-              const bf16x8_t pl = __builtin_bit_cast(bf16x8_t, make_uint4(lo[0][0], lo[0][1], lo[1][0], lo[1][1]));
+            if constexpr (decltype(fp32_c)::value) {
 #pragma unroll
-              for (int dt = 0; dt < 4; ++dt) {   // dims 32 dt + 2 r16 (acc[2 dt]) and + 1
-                unsigned ev[4], od[4];
+              for (int i = 0; i < 4; ++i)        // step i of the product: the keys 4 g + i, g = 0 .. 3
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                  const unsigned w = c == 0 ? vw[dt].x : c == 1 ? vw[dt].y : c == 2 ? vw[4 + dt].x : vw[4 + dt].y;
-                  const unsigned s = __builtin_amdgcn_perm(w, w, 0x03010200u);   // bytes: even dim of two keys, odd dim
-                  ev[c] = fp8_lo(s);
-                  od[c] = fp8_hi(s);
+                for (int dt = 0; dt < 8; ++dt) {
+                  const unsigned w = i & 2 ? vw[dt].y : vw[dt].x;
+                  acc[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(i & 1 ? hi_bf(w) : lo_bf(w), p[0][i], acc[nt][dt], 0, 0, 0);
                 }
-                const bf16x8_t ve = __builtin_bit_cast(bf16x8_t, make_uint4(ev[0], ev[1], ev[2], ev[3]));
-                const bf16x8_t vd = __builtin_bit_cast(bf16x8_t, make_uint4(od[0], od[1], od[2], od[3]));
-                acc[2 * dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, ph, acc[2 * dt], 0, 0, 0);
-                acc[2 * dt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vd, ph, acc[2 * dt + 1], 0, 0, 0);
-                acc[2 * dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, pl, acc[2 * dt], 0, 0, 0);
-                acc[2 * dt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vd, pl, acc[2 * dt + 1], 0, 0, 0);
-              }
-            } else {                             // one product takes both parts against the values twice
-              const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, make_uint4(hi[0][0], hi[0][1], lo[0][0], lo[0][1]));
+            } else if constexpr (!E4M3) {        // one product takes both parts against the values twice
+              const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, make_uint4(hi[nt][0][0], hi[nt][0][1], lo[nt][0][0], lo[nt][0][1]));
 #pragma unroll
               for (int dt = 0; dt < 8; ++dt) {
                 const bf16x8_t v2 = __builtin_bit_cast(bf16x8_t, make_uint4(vw[dt].x, vw[dt].y, vw[dt].x, vw[dt].y));
-                acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v2, pf, acc[dt], 0, 0, 0);
+                acc[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v2, pf, acc[nt][dt], 0, 0, 0);
+              }
+            }
+          }
+          if constexpr (E4M3) {                  // the 32 keys' first parts, then their second
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) {     // dims 32 dt + 2 r16 (acc[2 dt]) and + 1
+              unsigned ev[4], od[4];
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                const unsigned w = c == 0 ? vw[dt].x : c == 1 ? vw[dt].y : c == 2 ? vw[4 + dt].x : vw[4 + dt].y;
+                const unsigned s = __builtin_amdgcn_perm(w, w, 0x03010200u);   // bytes: even dim of two keys, odd dim
+                ev[c] = fp8_lo(s);
+                od[c] = fp8_hi(s);
+              }
+              const bf16x8_t ve = __builtin_bit_cast(bf16x8_t, make_uint4(ev[0], ev[1], ev[2], ev[3]));
+              const bf16x8_t vd = __builtin_bit_cast(bf16x8_t, make_uint4(od[0], od[1], od[2], od[3]));
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                const bf16x8_t ph = __builtin_bit_cast(bf16x8_t, make_uint4(hi[nt][0][0], hi[nt][0][1], hi[nt][HV - 1][0], hi[nt][HV - 1][1]));
+                const bf16x8_t pl = __builtin_bit_cast(bf16x8_t, make_uint4(lo[nt][0][0], lo[nt][0][1], lo[nt][HV - 1][0], lo[nt][HV - 1][1]));
+                acc[nt][2 * dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, ph, acc[nt][2 * dt], 0, 0, 0);
+                acc[nt][2 * dt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vd, ph, acc[nt][2 * dt + 1], 0, 0, 0);
+                acc[nt][2 * dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, pl, acc[nt][2 * dt], 0, 0, 0);
+                acc[nt][2 * dt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vd, pl, acc[nt][2 * dt + 1], 0, 0, 0);
               }
             }
           }
@@ -372,145 +426,171 @@ __global__ __launch_bounds__(64 * FNW) void paged_few_kernel(const PagedArgs a, 
       if constexpr (!E4M3) {
         bool odd = false;
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) odd |= !(fabsf(acc[dt][r]) < INFINITY);
+          for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) odd |= !(fabsf(acc[nt][dt][r]) < INFINITY);
         if (__any(odd)) {
           start();
           sweep(std::true_type{});
           wait_vmcnt<0>();
         }
       }
-      l += __shfl_xor(l, 16, 64);
-      l += __shfl_xor(l, 32, 64);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        l[nt] += __shfl_xor(l[nt], 16, 64);
+        l[nt] += __shfl_xor(l[nt], 32, 64);
+      }
 
       // ---- dims that a lane holds: 16 dt + 4 g + r of acc[dt][r]; e4m3: 32 (dt / 2) + 8 g + 2 r + dt % 2
-      auto at_dim = [&](int dt, int r) { return E4M3 ? 32 * (dt >> 1) + 8 * g + 2 * r + (dt & 1) : 16 * dt + 4 * g + r; };
-      const long long unit = base + u * nb;      // place of the unit's first block
-      const long long wg0 = (long long)blockIdx.x * FNW * per;
-      if (from == 0 && to == nb) {
-        if (row_ok) {
-          const float inv = l == 0.0f ? 0.0f : (E4M3 && a.v_scale ? a.v_scale[h] : 1.0f) / l;
-          bf16_t* dst = out + (qrow * a.hpr + head) * PHD;
+      const int rows = min(ROWS, n * grp - tile * ROWS);
+      auto put = [&](float* po, const f32x4_t* c) {   // a tile's sums as fp32 rows
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const f32x4_t x = c[2 * t], y = c[2 * t + 1];
+          float* at = po + r16 * FPR + 32 * t;
+          if constexpr (E4M3) {
+            *reinterpret_cast<f32x4_t*>(at + 8 * g) = f32x4_t{x[0], y[0], x[1], y[1]};
+            *reinterpret_cast<f32x4_t*>(at + 8 * g + 4) = f32x4_t{x[2], y[2], x[3], y[3]};
+          } else {
+            *reinterpret_cast<f32x4_t*>(at + 4 * g) = x;
+            *reinterpret_cast<f32x4_t*>(at + 16 + 4 * g) = y;
+          }
+        }
+      };
+      const float vs = E4M3 && a.v_scale ? a.v_scale[h] : 1.0f;
+      if (mode == FEW_WAVE || (mode == FEW_LINE && begins && to == unit + nb)) {
+        if (lane == 0 && unit0 + u < unit_joins) joins[unit0 + u].rows = 0;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          if (!row_ok[nt]) continue;
+          const float inv = l[nt] == 0.0f ? 0.0f : vs / l[nt];
+          bf16_t* dst = out + qat[nt] * PHD;
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
+            const f32x4_t x = acc[nt][2 * t], y = acc[nt][2 * t + 1];
             if constexpr (E4M3) {
-              uint4 w;
-              w.x = pack2bf(acc[2 * t][0] * inv, acc[2 * t + 1][0] * inv);
-              w.y = pack2bf(acc[2 * t][1] * inv, acc[2 * t + 1][1] * inv);
-              w.z = pack2bf(acc[2 * t][2] * inv, acc[2 * t + 1][2] * inv);
-              w.w = pack2bf(acc[2 * t][3] * inv, acc[2 * t + 1][3] * inv);
-              *reinterpret_cast<uint4*>(dst + 32 * t + 8 * g) = w;
+              *reinterpret_cast<uint4*>(dst + 32 * t + 8 * g) =
+                  make_uint4(pack2bf(x[0] * inv, y[0] * inv), pack2bf(x[1] * inv, y[1] * inv), pack2bf(x[2] * inv, y[2] * inv),
+                             pack2bf(x[3] * inv, y[3] * inv));
             } else {
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const int dt = 2 * t + k;
-                uint2 w;
-                w.x = pack2bf(acc[dt][0] * inv, acc[dt][1] * inv);
-                w.y = pack2bf(acc[dt][2] * inv, acc[dt][3] * inv);
-                *reinterpret_cast<uint2*>(dst + 16 * dt + 4 * g) = w;
-              }
+              *reinterpret_cast<uint2*>(dst + 32 * t + 4 * g) = make_uint2(pack2bf(x[0] * inv, x[1] * inv), pack2bf(x[2] * inv, x[3] * inv));
+              *reinterpret_cast<uint2*>(dst + 32 * t + 16 + 4 * g) = make_uint2(pack2bf(y[0] * inv, y[1] * inv), pack2bf(y[2] * inv, y[3] * inv));
             }
           }
         }
       } else {
-        if (from == 0) join = FewJoin{min(16, n * grp - tile * 16), rank, kvh, first, tile, 0, unit, unit + nb, per};
-        // all four stretches lie inside the unit: joined here, one partial result for the workgroup
-        const bool together = unit <= wg0 && wg0 + FNW * per <= unit + nb;
-        float* po = together ? reinterpret_cast<float*>(ring) + wave * FSLOT : part + (2LL * wid + (x == x0 ? 0 : 1)) * FSLOT;
-        if (together) __syncthreads();           // before the partial results take the rings' place
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) {
-          if constexpr (E4M3) {
-            if (dt & 1) continue;
-            *reinterpret_cast<f32x4_t*>(po + r16 * FPR + at_dim(dt, 0)) = f32x4_t{acc[dt][0], acc[dt + 1][0], acc[dt][1], acc[dt + 1][1]};
-            *reinterpret_cast<f32x4_t*>(po + r16 * FPR + at_dim(dt, 2)) = f32x4_t{acc[dt][2], acc[dt + 1][2], acc[dt][3], acc[dt + 1][3]};
-          } else {
-            *reinterpret_cast<f32x4_t*>(po + r16 * FPR + at_dim(dt, 0)) = acc[dt];
-          }
+        if (mode == FEW_LINE && begins) {
+          join = FewJoin{rows, rank, kvh, first, tile * ROWS, unit + FSTART, unit + nb, per};
+          if (lane == 0 && unit0 + u < unit_joins) joins[unit0 + u] = join;
         }
-        if (!together) {
-          if (g == 0) {
-            po[r16 * FPR + PHD] = m;
-            po[r16 * FPR + PHD + 1] = l;
+        const int wg0 = blockIdx.x * FNW * per;
+        if (mode == FEW_WG || (unit + FSTART <= wg0 && wg0 + FNW * per <= unit + nb)) {
+          // all four stretches lie inside the unit's blocks: joined here, one (partial) result for the workgroup
+          float* po = reinterpret_cast<float*>(ring);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            if (nt * 16 >= rows) break;
+            __syncthreads();                     // before the partial results take the rings' place, or the last tile's
+            put(po + wave * 16 * FPR, acc[nt]);
+            if (g == 0) {
+              s_m[wave][r16] = m[nt];
+              s_l[wave][r16] = l[nt];
+            }
+            __syncthreads();
+            float* dst = part + 2LL * blockIdx.x * FNW * FSLOT + nt * 16 * FPR;
+            const int here = min(16, rows - nt * 16);
+            for (int i = threadIdx.x; i < here * PHD; i += 64 * FNW) {
+              const int r = i / PHD, d = i - r * PHD;
+              float M = s_m[0][r];
+#pragma unroll
+              for (int w = 1; w < FNW; ++w) M = fmaxf(M, s_m[w][r]);
+              const float mb = M == -INFINITY ? 0.0f : M;
+              float num = 0.0f, den = 0.0f;
+#pragma unroll
+              for (int w = 0; w < FNW; ++w) {
+                const float f = __builtin_amdgcn_exp2f(s_m[w][r] - mb);
+                num += po[(w * 16 + r) * FPR + d] * f;
+                den += s_l[w][r] * f;
+              }
+              if (mode == FEW_WG) {
+                const int qr = tile * ROWS + nt * 16 + r, token = qr / grp, head = kvh * grp + (qr - token * grp);
+                out[(((long long)rank * a.rows + first + token) * a.hpr + head) * PHD + d] = f2bf(den == 0.0f ? 0.0f : num * (vs / den));
+                continue;
+              }
+              dst[r * FPR + d] = num;
+              if (d == 0) {
+                dst[r * FPR + PHD] = M;
+                dst[r * FPR + PHD + 1] = den;
+              }
+            }
           }
         } else {
-          if (g == 0) {
-            s_m[wave][r16] = m;
-            s_l[wave][r16] = l;
-          }
-          __syncthreads();
-          const float* pr = reinterpret_cast<const float*>(ring);
-          float* dst = part + 2LL * blockIdx.x * FNW * FSLOT;
-          const int rows = min(16, n * grp - tile * 16);
-          for (int i = threadIdx.x; i < rows * PHD; i += 64 * FNW) {
-            const int r = i / PHD, d = i - r * PHD;
-            float M = s_m[0][r];
+          float* po = part + (2LL * wid + (begins ? 1 : 0)) * FSLOT;
 #pragma unroll
-            for (int w = 1; w < FNW; ++w) M = fmaxf(M, s_m[w][r]);
-            const float mb = M == -INFINITY ? 0.0f : M;
-            float num = 0.0f, den = 0.0f;
-#pragma unroll
-            for (int w = 0; w < FNW; ++w) {
-              const float f = __builtin_amdgcn_exp2f(s_m[w][r] - mb);
-              num += pr[w * FSLOT + r * FPR + d] * f;
-              den += s_l[w][r] * f;
-            }
-            dst[r * FPR + d] = num;
-            if (d == 0) {
-              dst[r * FPR + PHD] = M;
-              dst[r * FPR + PHD + 1] = den;
+          for (int nt = 0; nt < NT; ++nt) {
+            put(po + nt * 16 * FPR, acc[nt]);
+            if (g == 0) {
+              po[(nt * 16 + r16) * FPR + PHD] = m[nt];
+              po[(nt * 16 + r16) * FPR + PHD + 1] = l[nt];
             }
           }
         }
       }
       // ---- the next unit
-      x += to - from;
+      x = to;
       if (x < x1 && x >= base + work * heads) {
         base += work * heads;
-        do {                                     // (some sequence behind this one has work: x < total)
-          ++b;
+        unit0 += tiles * heads;
+        while (++b < a.batch) {
           if (b >= sq.at + 64) sq = load_seqs(b);
-        } while (__builtin_amdgcn_readlane(sq.n, b - sq.at) == 0);
+          if (__builtin_amdgcn_readlane(sq.units, b - sq.at) > 0) break;
+        }
       }
     }
   }
-  if (joins && lane == 0) joins[wid] = join;
+  if (unit_joins) {                              // the launch has room for unit_joins units
+    for (int i = units + wid * 64 + lane; i < unit_joins; i += nwaves * 64) joins[i].rows = 0;
+  } else if (mode == FEW_LINE && lane == 0) {
+    joins[wid] = join;
+  }
 }
 
-// Joins the partial results of the units that cross stretches: a wave per (unit, row); blockIdx.x is the wave in which the unit
-// begins.  Their order is that of the keys: single waves up to the first whole workgroup, the workgroups, single waves.
+// Joins the partial results of the units that cross stretches: a wave per (unit, row).  Their order is that of the keys: single
+// waves up to the first whole workgroup, the workgroups, single waves.
 __global__ __launch_bounds__(64) void paged_few_join_kernel(const PagedArgs a, const float* __restrict__ part, const FewJoin* __restrict__ joins,
-                                                            bf16_t* __restrict__ out) {
+                                                            bf16_t* __restrict__ out, int slot_rows) {
   const FewJoin j = joins[blockIdx.x];
   if ((int)blockIdx.y >= j.rows) return;
   const int lane = threadIdx.x;
-  const long long per = j.per;
-  const int w0 = blockIdx.x, w1 = (int)((j.end - 1) / per);                       // waves of the unit
-  const int ga = (int)((j.begin + FNW * per - 1) / (FNW * per)), gb = (int)(j.end / (FNW * per));   // workgroups inside it
+  const long long wg = (long long)FNW * j.per;
+  const int w0 = j.begin / j.per, w1 = (j.end - 1) / j.per;                       // waves of the unit
+  const int ga = (int)((j.begin + wg - 1) / wg), gb = (int)(j.end / wg);          // workgroups inside it
   const int head = gb > ga ? ga * FNW - w0 : w1 + 1 - w0, mid = gb > ga ? gb - ga : 0;
   const int tail = gb > ga ? w1 + 1 - gb * FNW : 0, count = head + mid + tail;
   auto slot = [&](int i) -> long long {
-    if (i < head) return 2LL * (w0 + i) + ((w0 + i) * per < j.begin ? 1 : 0);
+    if (i < head) return 2LL * (w0 + i) + (i == 0 ? 1 : 0);   // the first one's lies behind that of the unit before
     if (i < head + mid) return 2LL * FNW * (ga + i - head);
     return 2LL * (gb * FNW + i - head - mid);
   };
   const int grp = a.hpr / a.kvpr;
   for (int r = blockIdx.y; r < j.rows; r += gridDim.y) {
     float M = -INFINITY, den = 0.0f, n0 = 0.0f, n1 = 0.0f;
-    for (int c0 = 0; c0 < count; c0 += 64) {
-      float pm = -INFINITY, pl = 0.0f;
-      long long at = 0;
-      if (c0 + lane < count) {
-        at = slot(c0 + lane) * FSLOT + r * FPR;
-        pm = part[at + PHD];
-        pl = part[at + PHD + 1];
-      }
+    auto take = [&](int c0, auto most_c) {       // partial results c0 .. c0 + MOST - 1, all loads under way at once
+      constexpr int MOST = decltype(most_c)::value;
+      const int here = min(MOST, count - c0);
+      const long long at = (slot(c0 + min(lane, here - 1)) * slot_rows + r) * FPR;
+      const float2 ml = *reinterpret_cast<const float2*>(part + at + PHD);
+      float2 v[MOST];
+#pragma unroll
+      for (int i = 0; i < MOST; ++i) v[i] = *reinterpret_cast<const float2*>(part + lane64(at, i) + lane * 2);
+      const float pm = lane < here ? ml.x : -INFINITY, pl = lane < here ? ml.y : 0.0f;
       float mx = pm;
 #pragma unroll
       for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, 64));
       const float m_new = fmaxf(M, mx), mb = m_new == -INFINITY ? 0.0f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(M - mb), f = __builtin_amdgcn_exp2f(pm - mb);
+      const float alpha = __builtin_amdgcn_exp2f(M - mb), f = lane < here ? __builtin_amdgcn_exp2f(pm - mb) : 0.0f;
       float sum = pl * f;
 #pragma unroll
       for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
@@ -518,48 +598,70 @@ __global__ __launch_bounds__(64) void paged_few_join_kernel(const PagedArgs a, c
       n0 *= alpha;
       n1 *= alpha;
       M = m_new;
-      const int here = min(64, count - c0);
-      for (int i0 = 0; i0 < here; i0 += 8) {
-        float2 v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          v[i] = i0 + i < here ? *reinterpret_cast<const float2*>(part + lane64(at, i0 + i) + lane * 2) : make_float2(0.0f, 0.0f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i0 + i));   // 0 behind the last
+      for (int i = 0; i < MOST; ++i) {
+        const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
+        if (i < here) {
           n0 += v[i].x * fi;
           n1 += v[i].y * fi;
         }
       }
-    }
-    const int qr = j.tile * 16 + r, token = qr / grp, h = j.kvh * grp + (qr - token * grp);
+    };
+    if (count <= 8) take(0, std::integral_constant<int, 8>{});
+    else
+      for (int c0 = 0; c0 < count; c0 += 32) take(c0, std::integral_constant<int, 32>{});
+    const int qr = j.row0 + r, token = qr / grp, h = j.kvh * grp + (qr - token * grp);
     const float inv = den == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[j.rank * a.kvpr + j.kvh] : 1.0f) / den;
     *reinterpret_cast<unsigned*>(out + (((long long)j.rank * a.rows + j.first + token) * a.hpr + h) * PHD + lane * 2) = pack2bf(n0 * inv, n1 * inv);
   }
 }
 
-size_t paged_few_workspace_bytes() {
-  return (size_t)FMAX_WGS * FNW * (sizeof(FewJoin) + 2 * FSLOT * sizeof(float));
+// Tiles of 16 query rows per unit: one read of K and V for all of them.  More would not fit the registers (in e4m3 the widened
+// fragments of K and V take 32 more); 49 to 64 rows go as two units of two tiles.
+static int few_tiles(const PagedArgs& a, int e4m3, int max_new) {
+  const long long rows = (long long)max_new * (a.hpr / a.kvpr);
+  return rows <= 16 ? 1 : rows > 32 && rows <= 48 && !e4m3 ? 3 : 2;
+}
+
+// at most as many units as this: a sequence's last tile is not full
+static long long few_units(const PagedArgs& a, int nt) {
+  const long long grp = a.hpr / a.kvpr;
+  return std::min((a.rows * grp + 16 * nt - 1) / (16 * nt) + a.batch - 1, a.rows * grp) * a.T * a.kvpr;
+}
+
+// 64 rows of queries and more go to the prompts' kernel; so does what would not leave the line's places 31 bits
+bool paged_few_takes(const PagedArgs& a, int e4m3, int max_new) {
+  const long long nb = ((long long)a.max_pages * a.page_size + 15) / 16 + FSTART;
+  return (long long)max_new * (a.hpr / a.kvpr) <= 64 && few_units(a, few_tiles(a, e4m3, max_new)) <= 0x7FFFFFFFLL / nb;
+}
+
+size_t paged_few_workspace_bytes(const PagedArgs& a, int e4m3, int max_new) {
+  return (size_t)FMAX_WGS * FNW * (sizeof(FewJoin) + 2 * few_tiles(a, e4m3, max_new) * 16 * FPR * sizeof(float));
 }
 
 hipError_t launch_paged_few(const PagedArgs& a, int e4m3, int max_new, const bf16_t* q, bf16_t* out, const void* kc, const void* vc,
                             void* workspace, hipStream_t s) {
   const long long grp = a.hpr / a.kvpr, cap = (long long)a.max_pages * a.page_size;
   const long long kb = e4m3 ? 32 : 16, nb = (cap + kb - 1) / kb;
-  const int whole = nb <= 4;                     // caches of so few keys are not worth a second kernel
-  const int least = whole ? 1 : 2;
-  const long long most = ((a.rows * grp + 15) / 16 + a.batch) * a.T * a.kvpr * (whole ? 1 : nb);   // blocks, at most
+  const int nt = few_tiles(a, e4m3, max_new);
+  const long long units = few_units(a, nt);
+  // A cache of so few keys that a wave does them in the time of a second kernel's launch, then one of so few that a workgroup
+  // does (and the launch has one for every unit)
+  const int mode = nb <= 4 ? FEW_WAVE : nb <= 8 * FNW && units <= FMAX_WGS ? FEW_WG : FEW_LINE;
+  const int least = mode == FEW_LINE ? 2 : 1;
+  const long long most = mode == FEW_WG ? units * FNW : mode == FEW_WAVE ? units : units * (nb + FSTART);
   const int wgs = (int)std::min<long long>(FMAX_WGS, (most + least * FNW - 1) / (least * FNW));
+  const int unit_joins = mode == FEW_LINE && units <= FMAX_WGS * FNW ? (int)units : 0;
   FewJoin* joins = reinterpret_cast<FewJoin*>(workspace);
   float* part = reinterpret_cast<float*>(joins + FMAX_WGS * FNW);
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)PHD);
-  auto kernel = e4m3 ? paged_few_kernel<true> : paged_few_kernel<false>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(64 * FNW), 0, s, a, q, out, kc, vc, part, whole ? nullptr : joins, scale_log2,
-                     least, whole);
+  auto kernel = e4m3 ? (nt == 1 ? paged_few_kernel<true, 1> : paged_few_kernel<true, 2>)
+                     : (nt == 1 ? paged_few_kernel<false, 1> : nt == 2 ? paged_few_kernel<false, 2> : paged_few_kernel<false, 3>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(64 * FNW), 0, s, a, q, out, kc, vc, part, joins, scale_log2, least, mode, unit_joins);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || whole) return e;
-  const int rows = (int)std::min<long long>(16, grp * max_new);
-  hipLaunchKernelGGL(paged_few_join_kernel, dim3((unsigned)(wgs * FNW), (unsigned)rows), dim3(64), 0, s, a, part, joins, out);
+  if (e != hipSuccess || mode != FEW_LINE) return e;
+  const int rows = (int)std::min<long long>(16 * nt, grp * max_new);
+  hipLaunchKernelGGL(paged_few_join_kernel, dim3((unsigned)(unit_joins ? unit_joins : wgs * FNW), (unsigned)rows), dim3(64), 0, s, a, part, joins, out, 16 * nt);
   return hipGetLastError();
 }
 

@@ -18,6 +18,15 @@ FEW_TOKENS = [
     (1, 8, 2, [100, 9, 0, 260], [5, 9, 0, 4], 16, False, "phrd"),            # drafts; 9 new of 9
     (1, 2, 2, [64, 200], [17, 3], 32, False, "phrd"),                        # 17 rows
     (1, 3, 1, [50, 4], [5, 4], 16, False, "phrd"),                           # 15 and 12 rows
+    (1, 16, 2, [300, 77, 50], [5, 6, 3], 16, False, "phrd"),                 # 40, 48 and 24 rows in tiles of 48
+    (1, 8, 1, [1500, 30, 9], [8, 7, 1], 16, False, "phrd"),                  # 64 and 56 rows
+    (1, 6, 1, [3001], [7], 64, False, "phrd"),                               # 42 rows, many workgroups inside one unit
+    (1, 8, 1, [2222, 40], [4, 3], 32, True, "phrd"),                         # 32 and 24 rows
+    (2, 4, 2, [(17 * i) % 311 for i in range(70)], [int(i % 9 != 0) for i in range(70)], 32, False, "phrd"),   # more than 64 sequences
+    (1, 8, 4, [(29 * i) % 801 + 1 for i in range(150)], [i % 3 for i in range(150)], 16, True, "phrd"),
+    (1, 2, 1, [5 + 40 * (i == 131) for i in range(200)], [1] * 200, 16, False, "phrd"),   # short sequences around one
+    (1, 2, 2, [1000, 200], [1, 1], 512, True, "phrd"),                       # a workgroup per unit
+    (8, 8, 8, [500], [1], 16, False, "phrd"),
     (1, 1, 1, [1], [1], 16, True, "phrd"),
     (2, 8, 2, [15, 16, 17, 31, 32, 33, 0, 1], [1, 1, 1, 1, 1, 1, 0, 1], 16, True, "phrd"),
     (1, 8, 1, [300, 1, 511, 64], [1, 2, 3, 2], 48, True, "prhd"),
@@ -128,6 +137,33 @@ def test_what_no_query_sees_does_not_matter(e4m3, new):
     P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.FEW if new <= 3 else P.MANY)
 
 
+@pytest.mark.parametrize("new", [1, 3, 6, 90])
+@pytest.mark.parametrize("long", [70, 1200])
+def test_infinities_that_are_seen(new, long):
+    """An infinite value gives infinities of its sign in its channel (NaN where both signs meet) and leaves the other channels
+    alone; an infinite key makes NaN of the rows that see it."""
+    c = P.make(22, 1, 16, 2, [long + new, new + 33], [new, new], 16)
+    w, k = P.view(c, c.v), P.view(c, c.k)
+    at = lambda b, t: (c.table[b, t // 16], t % 16)
+    (p0, o0), (p1, o1), (p2, o2) = at(0, 20), at(0, 37), at(1, 9)
+    w[0, p0, 0, o0, 5], w[0, p1, 0, o1, 6], w[0, p0, 0, o0, 7], w[0, p1, 0, o1, 7] = 0x7F80, 0xFF80, 0x7F80, 0xFF80
+    k[0, p2, 1, o2, 3] = 0x7F80
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    got = P.widen(P.bits(d.out)).reshape(1, -1, 16, 128)
+    with np.errstate(invalid="ignore"):
+        ref, size = (x.reshape(1, -1, 16, 128) for x in P.ref_attn(c))
+    assert np.all(got[0, :new, :8, 5] == np.inf) and np.all(got[0, :new, :8, 6] == -np.inf) and np.all(np.isnan(got[0, :new, :8, 7]))
+    with np.errstate(invalid="ignore"):
+        q = P.widen(c.q)[0, new:].reshape(-1, 16, 128)[:, 8:, 3]
+    assert np.all(np.isnan(got[0, new:, 8:]) | (q < 0)[:, :, None])          # + infinity: NaN; - infinity: a probability of 0
+    fine = np.ones(got.shape, dtype=bool)
+    fine[0, :new, :8, 5:8] = False
+    fine[0, new:, 8:] = False
+    got, ref, size = got[fine], ref[fine], size[fine]
+    assert np.all(np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + (P.FEW if new * 8 <= 64 else P.MANY) * size)
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("new", [1, 2, 90])
 def test_lists_that_are_wrong(e4m3, new):
@@ -148,7 +184,8 @@ def test_lists_that_are_wrong(e4m3, new):
     d = P.on_gpu(c)
     P.append(c, d)
     P.check_append(c, P.bits(d.q_out), P.bits(d.k), P.bits(d.v), c.k, c.v)
-    for wrong in ([-1, new, 2 * new, 3 * new, 4 * new, 5 * new, 6 * new], [0, new, new - 1, 2 ** 31 - 1, 4 * new, 4 * new, 6 * new + 2]):
+    for wrong in ([-1, new, 2 * new, 3 * new, 4 * new, 5 * new, 6 * new], [0, new, new - 1, 2 ** 31 - 1, 4 * new, 4 * new, 6 * new + 2],
+                  [0, 6 * new, 0, 6 * new, 0, 6 * new, 0], [0] + [6 * new] * 6):
         d = P.on_gpu(c)
         import torch
         d.row_start = torch.tensor(wrong, dtype=torch.int32, device="cuda")
