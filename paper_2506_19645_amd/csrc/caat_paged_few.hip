@@ -35,7 +35,8 @@ static constexpr int FMAX_WGS = 512;             // workgroups of a launch
 struct FewJoin {
   int rows;                                      // 0: the unit was finished by that wave
   int rank, kvh, first, row0;                    // row0: the unit's first (token, head) row of the sequence
-  int begin, end, per;                           // the unit's blocks in the line of all of them; length of a stretch
+  int begin, end, per;                           // the unit's blocks in the line of all of them; length of a stretch, negative:
+                                                 // of a workgroup
 };
 
 // Swizzles of the 16-byte chunks of a row in LDS (256-byte rows in bf16, 128 in e4m3): K is read 16 rows x one chunk at a
@@ -68,11 +69,13 @@ __device__ __forceinline__ int wave_sums(int v) {
 }
 
 // How the units are dealt out.  FEW_LINE: as the head of this file says.  FEW_WAVE: whole units to waves, FEW_WG: a unit to a
-// workgroup, a quarter of its blocks to each wave; neither leaves anything for the second kernel.
+// workgroup; neither leaves anything for the second kernel.
 enum FewMode { FEW_LINE = 0, FEW_WAVE = 1, FEW_WG = 2 };
-// A unit's start (its queries' and pages' way, the first block's, its results) takes about as long as this many blocks: it
-// stands in the line in front of them.
+// A unit's start (its queries' and pages' way, the first block's, its results) takes a wave about as long as FSTART blocks: they
+// stand in the line in front of the unit's own.  While there are at most FWIDE units, a stretch belongs to a workgroup, whose
+// waves take a quarter of its blocks each and join their results in LDS, so that a quarter as many go through the workspace.
 static constexpr int FSTART = 3;
+static constexpr int FWIDE = 24;
 
 // NT: tiles of 16 query rows of a unit, which share the fragments of K and V
 template <bool E4M3, int NT>
@@ -98,7 +101,7 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
   const int cap = a.max_pages * a.page_size;
 
   // ---- the line of all blocks, and this wave's stretch of it
-  auto load_seqs = [&](int at) {
+  auto load_seqs = [&](int at, int start_blocks) {
     SeqChunk c;
     c.at = at;
     c.first = c.n = c.len = c.units = 0;
@@ -106,25 +109,30 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
     if (at + lane < a.batch) {
       c.n = seq_rows(a, at + lane, c.first);
       c.len = max(a.lens[at + lane], 0);
-      const int nb = mode == FEW_LINE ? (min(c.len, cap) + KB - 1) / KB + FSTART : 1;
+      const int nb = mode == FEW_LINE ? (min(c.len, cap) + KB - 1) / KB + start_blocks : 1;
       c.units = (int)(((long long)c.n * grp + ROWS - 1) / ROWS);
       c.work = c.units * nb;
     }
     return c;
   };
-  SeqChunk sq = load_seqs(0);
-  int work_to = wave_sums(sq.work), units_to = wave_sums(sq.units);
-  int total = __builtin_amdgcn_readlane(work_to, 63), units = __builtin_amdgcn_readlane(units_to, 63);
+  SeqChunk sq = load_seqs(0, 0);
+  int units_to = wave_sums(sq.units), work_to = wave_sums(sq.work);
+  int units = __builtin_amdgcn_readlane(units_to, 63), total = __builtin_amdgcn_readlane(work_to, 63);
   for (int at = 64; at < a.batch; at += 64) {
-    const SeqChunk c = load_seqs(at);
-    total += __builtin_amdgcn_readlane(wave_sums(c.work), 63);
+    const SeqChunk c = load_seqs(at, 0);
     units += __builtin_amdgcn_readlane(wave_sums(c.units), 63);
+    total += __builtin_amdgcn_readlane(wave_sums(c.work), 63);
   }
-  total *= heads;                                // (the host has checked that this is below 2^31)
-  units *= heads;
-  const int nwaves = gridDim.x * FNW;
-  const int per = mode == FEW_WG ? 1 : max((int)((unsigned)(total + nwaves - 1) / (unsigned)nwaves), least);
-  const int x0 = (int)min((long long)(mode == FEW_WG ? blockIdx.x : wid) * per, (long long)total), x1 = min(total - x0, per) + x0;
+  units *= heads;                                // (the host has checked that the line has less than 2^31 places)
+  total *= heads;
+  const bool wide = mode == FEW_WG || (mode == FEW_LINE && total >= (long long)units * FWIDE);
+  const int start_blocks = mode == FEW_LINE ? (wide ? FSTART * FNW : FSTART) : 0;
+  total += units * start_blocks;
+  sq.work += sq.units * start_blocks;
+  work_to += units_to * start_blocks;
+  const int takers = wide ? gridDim.x : gridDim.x * FNW, taker = wide ? blockIdx.x : wid;
+  const int per = mode == FEW_WG ? 1 : max((int)((unsigned)(total + takers - 1) / (unsigned)takers), wide ? least * FNW : least);
+  const int x0 = (int)min((long long)taker * per, (long long)total), x1 = min(total - x0, per) + x0;
   FewJoin join = {};
   if (x0 < x1) {
     // the sequence of place x0: `base` is where its first unit begins, unit0 the number of that unit.  (There is one, unless the
@@ -141,7 +149,7 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
       }
       base += __builtin_amdgcn_readlane(work_to, 63) * heads;
       unit0 += __builtin_amdgcn_readlane(units_to, 63) * heads;
-      sq = load_seqs(sq.at + 64);
+      sq = load_seqs(sq.at + 64, start_blocks);
       work_to = wave_sums(sq.work);
       units_to = wave_sums(sq.units);
     }
@@ -155,26 +163,26 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
       const int tiles = __builtin_amdgcn_readlane(sq.units, sl);
       const int keys = min(len, cap);
       const int nblk = (keys + KB - 1) / KB;     // may be 0
-      const int nb = mode == FEW_LINE ? nblk + FSTART : 1;
+      const int nb = mode == FEW_LINE ? nblk + start_blocks : 1;
       const int u = (int)((unsigned)(x - base) / (unsigned)nb);
       const int unit = base + u * nb;            // place of the unit
       const int to = min(unit + nb, x1);         // and of the stretch's part of it: x .. to - 1
       const int h = (int)((unsigned)u / (unsigned)tiles), tile = u - h * tiles;
       const int rank = h / a.kvpr, kvh = h - rank * a.kvpr;
       // its blocks of keys
-      int k0, k1;
+      int k0 = 0, k1 = nblk;
       if (mode == FEW_LINE) {
-        k0 = max(x - unit - FSTART, 0);
-        k1 = max(to - unit - FSTART, 0);
+        k0 = max(x - unit - start_blocks, 0);
+        k1 = max(to - unit - start_blocks, 0);
         if (to < unit + nb && k1 == 0) break;    // the stretch ends in front of the first one
-      } else if (mode == FEW_WAVE) {
-        k0 = 0;
-        k1 = nblk;
-      } else {
-        k0 = nblk * wave / FNW;
-        k1 = nblk * (wave + 1) / FNW;
       }
-      const bool begins = unit + FSTART >= x0;   // FEW_LINE: its first block lies in this stretch
+      if (wide) {
+        const int all = k1 - k0, from = k0;
+        k0 = from + (int)((long long)all * wave / FNW);
+        k1 = from + (int)((long long)all * (wave + 1) / FNW);
+      }
+      const bool begins = unit + start_blocks >= x0;   // its first block lies in this stretch
+      const bool all_here = begins && to == unit + nb;
 
       // ---- pages: the table's entries from the first one on
       auto take_pages = [&](int col) {
@@ -460,8 +468,12 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
         }
       };
       const float vs = E4M3 && a.v_scale ? a.v_scale[h] : 1.0f;
-      if (mode == FEW_WAVE || (mode == FEW_LINE && begins && to == unit + nb)) {
-        if (lane == 0 && unit0 + u < unit_joins) joins[unit0 + u].rows = 0;
+      if (lane == 0 && unit0 + u < unit_joins && begins) {
+        FewJoin* j = joins + unit0 + u;
+        if (all_here) j->rows = 0;
+        else *j = FewJoin{rows, rank, kvh, first, tile * ROWS, unit + start_blocks, unit + nb, wide ? -per : per};
+      }
+      if (!wide && all_here) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           if (!row_ok[nt]) continue;
@@ -481,13 +493,10 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
           }
         }
       } else {
-        if (mode == FEW_LINE && begins) {
-          join = FewJoin{rows, rank, kvh, first, tile * ROWS, unit + FSTART, unit + nb, per};
-          if (lane == 0 && unit0 + u < unit_joins) joins[unit0 + u] = join;
-        }
+        if (begins && !all_here) join = FewJoin{rows, rank, kvh, first, tile * ROWS, unit + start_blocks, unit + nb, per};
         const int wg0 = blockIdx.x * FNW * per;
-        if (mode == FEW_WG || (unit + FSTART <= wg0 && wg0 + FNW * per <= unit + nb)) {
-          // all four stretches lie inside the unit's blocks: joined here, one (partial) result for the workgroup
+        if (wide || (unit + start_blocks <= wg0 && wg0 + FNW * per <= unit + nb)) {
+          // the workgroup's waves all work at this unit: joined here, one (partial) result
           float* po = reinterpret_cast<float*>(ring);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
@@ -499,7 +508,7 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
               s_l[wave][r16] = l[nt];
             }
             __syncthreads();
-            float* dst = part + 2LL * blockIdx.x * FNW * FSLOT + nt * 16 * FPR;
+            float* dst = part + (2LL * blockIdx.x * FNW + (wide && begins ? 1 : 0)) * FSLOT + nt * 16 * FPR;
             const int here = min(16, rows - nt * 16);
             for (int i = threadIdx.x; i < here * PHD; i += 64 * FNW) {
               const int r = i / PHD, d = i - r * PHD;
@@ -514,7 +523,7 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
                 num += po[(w * 16 + r) * FPR + d] * f;
                 den += s_l[w][r] * f;
               }
-              if (mode == FEW_WG) {
+              if (wide && all_here) {
                 const int qr = tile * ROWS + nt * 16 + r, token = qr / grp, head = kvh * grp + (qr - token * grp);
                 out[(((long long)rank * a.rows + first + token) * a.hpr + head) * PHD + d] = f2bf(den == 0.0f ? 0.0f : num * (vs / den));
                 continue;
@@ -544,14 +553,14 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
         base += work * heads;
         unit0 += tiles * heads;
         while (++b < a.batch) {
-          if (b >= sq.at + 64) sq = load_seqs(b);
+          if (b >= sq.at + 64) sq = load_seqs(b, start_blocks);
           if (__builtin_amdgcn_readlane(sq.units, b - sq.at) > 0) break;
         }
       }
     }
   }
   if (unit_joins) {                              // the launch has room for unit_joins units
-    for (int i = units + wid * 64 + lane; i < unit_joins; i += nwaves * 64) joins[i].rows = 0;
+    for (int i = units + wid * 64 + lane; i < unit_joins; i += gridDim.x * FNW * 64) joins[i].rows = 0;
   } else if (mode == FEW_LINE && lane == 0) {
     joins[wid] = join;
   }
@@ -564,13 +573,24 @@ __global__ __launch_bounds__(64) void paged_few_join_kernel(const PagedArgs a, c
   const FewJoin j = joins[blockIdx.x];
   if ((int)blockIdx.y >= j.rows) return;
   const int lane = threadIdx.x;
-  const long long wg = (long long)FNW * j.per;
-  const int w0 = j.begin / j.per, w1 = (j.end - 1) / j.per;                       // waves of the unit
-  const int ga = (int)((j.begin + wg - 1) / wg), gb = (int)(j.end / wg);          // workgroups inside it
-  const int head = gb > ga ? ga * FNW - w0 : w1 + 1 - w0, mid = gb > ga ? gb - ga : 0;
-  const int tail = gb > ga ? w1 + 1 - gb * FNW : 0, count = head + mid + tail;
-  auto slot = [&](int i) -> long long {
-    if (i < head) return 2LL * (w0 + i) + (i == 0 ? 1 : 0);   // the first one's lies behind that of the unit before
+  int head, mid, tail, w0, ga = 0, gb = 0;
+  if (j.per < 0) {                               // workgroups only
+    w0 = j.begin / -j.per;
+    head = (j.end - 1) / -j.per + 1 - w0;
+    mid = tail = 0;
+  } else {
+    const long long wg = (long long)FNW * j.per;
+    const int w1 = (j.end - 1) / j.per;
+    w0 = j.begin / j.per;                        // to w1: waves of the unit
+    ga = (int)((j.begin + wg - 1) / wg);         // to gb - 1: workgroups inside it
+    gb = (int)(j.end / wg);
+    head = gb > ga ? ga * FNW - w0 : w1 + 1 - w0;
+    mid = gb > ga ? gb - ga : 0;
+    tail = gb > ga ? w1 + 1 - gb * FNW : 0;
+  }
+  const int count = head + mid + tail;
+  auto slot = [&](int i) -> long long {          // the first one's lies behind that of the unit before
+    if (i < head) return 2LL * (w0 + i) * (j.per < 0 ? FNW : 1) + (i == 0 ? 1 : 0);
     if (i < head + mid) return 2LL * FNW * (ga + i - head);
     return 2LL * (gb * FNW + i - head - mid);
   };
@@ -631,7 +651,7 @@ static long long few_units(const PagedArgs& a, int nt) {
 
 // 64 rows of queries and more go to the prompts' kernel; so does what would not leave the line's places 31 bits
 bool paged_few_takes(const PagedArgs& a, int e4m3, int max_new) {
-  const long long nb = ((long long)a.max_pages * a.page_size + 15) / 16 + FSTART;
+  const long long nb = ((long long)a.max_pages * a.page_size + 15) / 16 + FSTART * FNW;
   return (long long)max_new * (a.hpr / a.kvpr) <= 64 && few_units(a, few_tiles(a, e4m3, max_new)) <= 0x7FFFFFFFLL / nb;
 }
 
@@ -649,7 +669,7 @@ hipError_t launch_paged_few(const PagedArgs& a, int e4m3, int max_new, const bf1
   // does (and the launch has one for every unit)
   const int mode = nb <= 4 ? FEW_WAVE : nb <= 8 * FNW && units <= FMAX_WGS ? FEW_WG : FEW_LINE;
   const int least = mode == FEW_LINE ? 2 : 1;
-  const long long most = mode == FEW_WG ? units * FNW : mode == FEW_WAVE ? units : units * (nb + FSTART);
+  const long long most = mode == FEW_WG ? units * FNW : mode == FEW_WAVE ? units : units * (nb + FSTART * FNW);
   const int wgs = (int)std::min<long long>(FMAX_WGS, (most + least * FNW - 1) / (least * FNW));
   const int unit_joins = mode == FEW_LINE && units <= FMAX_WGS * FNW ? (int)units : 0;
   FewJoin* joins = reinterpret_cast<FewJoin*>(workspace);
