@@ -31,6 +31,15 @@ static constexpr int PBK = 64;                   // keys per block
 static constexpr int PCH = PHD / 8;              // 16-byte chunks per row of a tile
 static constexpr int PTILE = PBK * PCH;          // chunks of a tile
 static constexpr int PRAW = 4 * 256;             // chunks of the waves' e4m3 buffers: 2 KB of K and 2 KB of V each
+static constexpr int PPR = PHD + 4;              // floats of a partial row: 128 sums, maximum, denominator, 2 unused
+static constexpr int PWGS = 512;                 // workgroups that run at a time
+
+// A tile whose keys are dealt to several workgroups: what the first of them says to the kernel that joins their results
+struct PromptJoin {
+  int rows;                                      // 0: nothing to join
+  int rank, kvh, first, row0;
+  int unused[3];
+};
 
 __device__ __forceinline__ int pk_swz(int row, int c) { return c ^ (row & 15); }
 __device__ __forceinline__ int pv_swz(int row, int c) { return c ^ ((row & 3) << 2); }
@@ -43,7 +52,8 @@ __device__ __forceinline__ float pmax3(float a, float b, float c) {
 
 template <bool E4M3>
 __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a, const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
-                                                              const void* __restrict__ kc, const void* __restrict__ vc, float scale_log2) {
+                                                              const void* __restrict__ kc, const void* __restrict__ vc,
+                                                              float* __restrict__ part, PromptJoin* __restrict__ joins, float scale_log2) {
   constexpr int ELT = E4M3 ? 1 : 2;
   __shared__ uint4 smem[4 * PTILE + (E4M3 ? PRAW : 0)];   // K slots 0 and 1, V slots 0 and 1, 16 KB each; e4m3 buffers
   const int tid = threadIdx.x, lane = tid & 63;
@@ -77,7 +87,11 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
       tile -= __builtin_amdgcn_readlane(incl, 63);
     }
   }
-  if (b < 0) return;                             // fewer tiles than the launch has room for
+  const int splits = gridDim.y, split = blockIdx.y;
+  if (b < 0) {                                   // fewer tiles than the launch has room for
+    if (splits > 1 && split == 0 && tid == 0) joins[blockIdx.x].rows = 0;
+    return;
+  }
   const int rank = h / a.kvpr, kvh = h - rank * a.kvpr;
   const int len = max(uni(a.lens[b]), 0);
   const int cap = a.max_pages * a.page_size;
@@ -86,7 +100,10 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
   const int row0 = tile * PBQ;
   const int last_token = min(n - 1, (row0 + PBQ - 1) / grp);
   const int kv_end = (int)min((long long)keys, (long long)len - n + last_token + 1);   // may be 0 or less
-  const int nblk = max(0, (kv_end + PBK - 1) / PBK);
+  const int all_blk = max(0, (kv_end + PBK - 1) / PBK);
+  const int blk0 = (int)((long long)all_blk * split / splits);   // this workgroup's share: blocks blk0 .. blk0 + nblk - 1
+  const int nblk = (int)((long long)all_blk * (split + 1) / splits) - blk0;
+  const int key0 = blk0 * PBK;
 
   // ---- Q fragments: B operand of S^T = K q^T: lane (row frow, k-half hf) holds q[16 ks + 8 hf .. + 7]
   const int qr = row0 + wave * 32 + frow;
@@ -120,7 +137,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
   // places are made from them when its K is copied and kept for its V, one block later.
   const const_i_t table = (const_i_t)(a.table + (long long)b * a.max_pages);
   const int gpp = a.page_size >> 4;              // groups per page
-  int next[4], ncol = 0, nin = 0;                // entries, and column and group inside the page behind them
+  int next[4], ncol = blk0 * 4 / gpp, nin = blk0 * 4 - ncol * gpp;   // entries, and column and group inside the page behind them
   auto fetch = [&] {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -135,7 +152,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
     long long at[4];                             // byte offsets of the groups inside a head's pages
     unsigned have;                               // groups that have a page
   };
-  int pin = 0;                                   // group inside its page of the block that is placed next
+  int pin = nin;                                 // group inside its page of the block that is placed next
   auto place = [&] {
     Place p;
     p.have = 0;
@@ -164,14 +181,14 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
   auto issue_rows = [&](const unsigned char* base, unsigned off, const Place& p, int blk, uint4* t) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int left = p.have >> i & 1 ? kv_end - blk * PBK - i * 16 : 0;   // rows of the group that anybody sees
+      const int left = p.have >> i & 1 ? kv_end - key0 - blk * PBK - i * 16 : 0;   // rows of the group that anybody sees
       const i32x4_t rs = make_rsrc(base + p.at[i]);
       dma16(rs, wave * 4 + (lane >> 4) < left ? off : 0x80000000u, t + (i * 16 + wave * 4) * PCH);
     }
   };
   uint4* raw = smem + 4 * PTILE + (E4M3 ? wave * 256 : 0);
   auto issue_raw = [&](const unsigned char* base, const Place& p, int blk, uint4* t) {   // the wave's group
-    const int left = p.have >> wave & 1 ? kv_end - blk * PBK - wave * 16 : 0;
+    const int left = p.have >> wave & 1 ? kv_end - key0 - blk * PBK - wave * 16 : 0;
     const long long at = wave == 0 ? p.at[0] : wave == 1 ? p.at[1] : wave == 2 ? p.at[2] : p.at[3];
     const i32x4_t rs = make_rsrc(base + at);
 #pragma unroll
@@ -252,7 +269,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
       }
       if (blk + 1 < nblk) issue_rows(vh, dvo, pv, blk + 1, vslot(blk + 1));
     }
-    const int kv0 = blk * PBK;
+    const int kv0 = key0 + blk * PBK;
     // ---- mask (keys of register r: kv0 + 32 j + 8 (r / 4) + 4 hf + r % 4): only where some row of the wave does not see the whole
     // block, or a group has no page
     if (kv0 + PBK > wave_lim || have != 15u) {
@@ -412,6 +429,20 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
 
   // ---- normalise and store: lane holds out[row][32 dt + 8 (r / 4) + 4 hf + r % 4]
   l_run += __shfl_xor(l_run, 32, 64);
+  if (splits > 1) {
+    if (split == 0 && tid == 0) joins[blockIdx.x] = PromptJoin{min(PBQ, n * grp - row0), rank, kvh, first, row0, {0, 0, 0}};
+    if (row_ok) {
+      float* o = part + (((long long)blockIdx.x * splits + split) * PBQ + wave * 32 + frow) * PPR;
+#pragma unroll
+      for (int dt = 0; dt < PHD / 32; ++dt)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          *reinterpret_cast<float4*>(o + dt * 32 + k * 8 + hf * 4) =
+              make_float4(oacc[dt][k * 4], oacc[dt][k * 4 + 1], oacc[dt][k * 4 + 2], oacc[dt][k * 4 + 3]);
+      if (hf == 0) *reinterpret_cast<float2*>(o + PHD) = make_float2(m_run * scale_log2, l_run);
+    }
+    return;
+  }
   if (row_ok) {
     const float inv = l_run == 0.0f ? 0.0f : (E4M3 && a.v_scale ? a.v_scale[h] : 1.0f) / l_run;
     bf16_t* o = out + (qrow * a.hpr + head) * PHD;
@@ -427,12 +458,84 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
   }
 }
 
-hipError_t launch_paged_prompt(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, hipStream_t s) {
-  const long long grp = a.hpr / a.kvpr;
-  const long long tiles = std::min<long long>(a.rows * grp / PBQ + a.batch, a.rows * grp);   // at most: one per sequence is not full
+// Joins the shares of a tile's keys, in their order: 32 threads per row, 4 channels each.
+__global__ __launch_bounds__(256) void paged_prompt_join_kernel(const PagedArgs a, const float* __restrict__ part,
+                                                                const PromptJoin* __restrict__ joins, bf16_t* __restrict__ out, int splits) {
+  const PromptJoin j = joins[blockIdx.x];
+  const int r = blockIdx.y * 8 + (threadIdx.x >> 5), c = (threadIdx.x & 31) * 4;
+  if (r >= j.rows) return;
+  const float* p = part + ((long long)blockIdx.x * splits * PBQ + r) * PPR;
+  float M = -INFINITY, den = 0.0f;
+  float4 num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int s0 = 0; s0 < splits; s0 += 4) {
+    float2 ml[4];
+    float4 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float* q = p + (long long)min(s0 + i, splits - 1) * PBQ * PPR;
+      ml[i] = *reinterpret_cast<const float2*>(q + PHD);
+      v[i] = *reinterpret_cast<const float4*>(q + c);
+      if (s0 + i >= splits) ml[i].x = -INFINITY;
+    }
+    const float m_new = fmaxf(fmaxf(M, ml[0].x), fmaxf(fmaxf(ml[1].x, ml[2].x), ml[3].x)), mb = m_new == -INFINITY ? 0.0f : m_new;
+    const float alpha = __builtin_amdgcn_exp2f(M - mb);
+    M = m_new;
+    den *= alpha;
+    num = make_float4(num.x * alpha, num.y * alpha, num.z * alpha, num.w * alpha);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (s0 + i >= splits) break;
+      const float f = __builtin_amdgcn_exp2f(ml[i].x - mb);
+      den += ml[i].y * f;
+      num = make_float4(num.x + v[i].x * f, num.y + v[i].y * f, num.z + v[i].z * f, num.w + v[i].w * f);
+    }
+  }
+  const int grp = a.hpr / a.kvpr, qr = j.row0 + r, token = qr / grp, h = j.kvh * grp + (qr - token * grp);
+  const float inv = den == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[j.rank * a.kvpr + j.kvh] : 1.0f) / den;
+  *reinterpret_cast<uint2*>(out + (((long long)j.rank * a.rows + j.first + token) * a.hpr + h) * PHD + c) =
+      make_uint2(pack2bf(num.x * inv, num.y * inv), pack2bf(num.z * inv, num.w * inv));
+}
+
+// at most as many tiles (of all heads) as this: a sequence's last one is not full
+static long long prompt_tiles(const PagedArgs& a) {
+  const long long rows = (long long)a.rows * (a.hpr / a.kvpr);
+  return std::min((rows + PBQ - 1) / PBQ + a.batch - 1, rows) * a.T * a.kvpr;
+}
+
+// Workgroups per tile.  Few tiles over many keys leave compute units idle; a share of the keys costs about 5 blocks' time more (its
+// start, its results' way through memory).  The host knows the table's width, not the lengths.
+static int prompt_splits(const PagedArgs& a) {
+  const long long tiles = prompt_tiles(a), nb = ((long long)a.max_pages * a.page_size + PBK - 1) / PBK;
+  int best = 1;
+  double cost = 0.0;
+  for (int s = 1; s <= 64 && (s == 1 || (tiles * s <= 2 * PWGS && nb / s >= 8)); ++s) {
+    const double c = (double)((tiles * s + PWGS - 1) / PWGS) * ((double)((nb + s - 1) / s) + (s > 1 ? 5.0 : 0.0));
+    if (s == 1 || c < cost) {
+      cost = c;
+      best = s;
+    }
+  }
+  return best;
+}
+
+size_t paged_prompt_workspace_bytes(const PagedArgs& a) {
+  const long long tiles = prompt_tiles(a);       // (whatever the table's width: the largest number of shares)
+  const long long shares = tiles > PWGS ? 0 : std::min<long long>(64, 2 * PWGS / tiles);
+  return shares < 2 ? 0 : (size_t)tiles * (sizeof(PromptJoin) + shares * PBQ * PPR * sizeof(float));
+}
+
+hipError_t launch_paged_prompt(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, void* workspace,
+                               hipStream_t s) {
+  const long long tiles = prompt_tiles(a);
+  const int splits = prompt_splits(a);
+  PromptJoin* joins = reinterpret_cast<PromptJoin*>(workspace);
+  float* part = reinterpret_cast<float*>(joins + tiles);
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)PHD);
   auto kernel = e4m3 ? paged_prompt_kernel<true> : paged_prompt_kernel<false>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles * a.T * a.kvpr)), dim3(256), 0, s, a, q, out, kc, vc, scale_log2);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)splits), dim3(256), 0, s, a, q, out, kc, vc, part, joins, scale_log2);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || splits == 1) return e;
+  hipLaunchKernelGGL(paged_prompt_join_kernel, dim3((unsigned)tiles, PBQ / 8), dim3(256), 0, s, a, part, joins, out, splits);
   return hipGetLastError();
 }
 

@@ -42,6 +42,9 @@ PROMPTS = [
     (2, 8, 2, [200, 77], [200, 50], 16, True, "phrd"),
     (1, 3, 1, [500, 2, 90], [257, 2, 90], 48, True, "prhd"),
     (1, 2, 2, [1000], [130], 128, True, "phrd"),
+    (1, 2, 1, [3001, 500, 0, 33], [70, 40, 0, 33], 16, False, "phrd"),       # the keys of a tile dealt to many workgroups,
+    (2, 4, 2, [2500, 90], [90, 90], 48, True, "phrd"),                       # of a short sequence to some that have none
+    (1, 8, 1, [5000], [300], 256, False, "prhd"),
 ]
 
 
