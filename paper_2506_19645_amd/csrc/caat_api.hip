@@ -865,7 +865,7 @@ size_t caat_paged_attn_workspace_bytes(const caat_paged_desc* d) {
   PagedArgs a;
   static const int some = 0;   // stands for a table of rows: a batch may have sequences without any
   if (paged_args(d, &some, nullptr, nullptr, nullptr, nullptr, &a) != CAAT_OK) return 0;
-  return paged_attn_workspace_bytes(a, d->cache_type == CAAT_CACHE_E4M3, d->max_new);
+  return paged_attn_workspace_bytes(a, d->max_new);
 }
 
 int caat_paged_attn(const caat_paged_desc* d, const void* q, void* out, const int* row_start, const int* lens,
@@ -875,7 +875,7 @@ int caat_paged_attn(const caat_paged_desc* d, const void* q, void* out, const in
   const int st = paged_args(d, row_start, lens, page_table, k_scale, v_scale, &a);
   if (st != CAAT_OK) return st;
   if (d->rows == 0) return CAAT_OK;
-  const size_t need = paged_attn_workspace_bytes(a, d->cache_type == CAAT_CACHE_E4M3, d->max_new);
+  const size_t need = paged_attn_workspace_bytes(a, d->max_new);
   if (!q || !out || !lens || !page_table || !k_cache || !v_cache || (need > 0 && !workspace)) return CAAT_EINVAL;
   if (misaligned(q) || misaligned(out) || paged_misaligned(a, k_cache, v_cache) || (need > 0 && misaligned(workspace)))
     return CAAT_EALIGN;

@@ -391,7 +391,7 @@ struct PagedArgs {
 };
 hipError_t launch_paged_append(const PagedArgs& a, int e4m3, const bf16_t* qkv, bf16_t* q_out, long long ld_qkv, void* kc, void* vc,
                                float rope_base, hipStream_t s);
-size_t paged_attn_workspace_bytes(const PagedArgs& a, int e4m3, int max_new);
+size_t paged_attn_workspace_bytes(const PagedArgs& a, int max_new);
 hipError_t launch_paged_attn(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, int max_new,
                              void* workspace, hipStream_t s);
 

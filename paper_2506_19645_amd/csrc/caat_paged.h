@@ -27,8 +27,8 @@ __device__ __forceinline__ long long lane64(long long x, int lane) {   // a lane
 }
 
 // The two forms of the attention: caat_paged_few.hip, caat_paged_prompt.hip
-bool paged_few_takes(const PagedArgs& a, int e4m3, int max_new);
-size_t paged_few_workspace_bytes(const PagedArgs& a, int e4m3, int max_new);
+bool paged_few_takes(const PagedArgs& a, int max_new);
+size_t paged_few_workspace_bytes(const PagedArgs& a, int max_new);
 hipError_t launch_paged_few(const PagedArgs& a, int e4m3, int max_new, const bf16_t* q, bf16_t* out, const void* kc, const void* vc,
                             void* workspace, hipStream_t s);
 size_t paged_prompt_workspace_bytes(const PagedArgs& a);

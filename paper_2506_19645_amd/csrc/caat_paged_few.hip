@@ -1,6 +1,6 @@
 // Attention of few new tokens per sequence (decode steps, drafted tokens) over a paged key / value cache, gfx950.
 //
-// What bounds it: the K / V rows, read once from HBM.  The unit of work is up to three tiles of 16 (token, query head of the group)
+// What bounds it: the K / V rows, read once from HBM.  The unit of work is one or two tiles of 16 (token, query head of the group)
 // rows of one sequence, rank and key / value head, times a block of keys (16 in bf16, 32 in e4m3: 8 KB of K and V).  The blocks of
 // all units stand in one line, sequence by sequence, and every WAVE of the launch takes an equal stretch of it, so a batch of
 // one long and many short sequences fills the chip like an even one, whatever the lengths (which only the device
@@ -535,6 +535,7 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
               }
             }
           }
+          __syncthreads();                       // before the next unit's blocks take the partial results' place
         } else {
           float* po = part + (2LL * wid + (begins ? 1 : 0)) * FSLOT;
 #pragma unroll
@@ -636,34 +637,33 @@ __global__ __launch_bounds__(64) void paged_few_join_kernel(const PagedArgs a, c
   }
 }
 
-// Tiles of 16 query rows per unit: one read of K and V for all of them.  More would not fit the registers (in e4m3 the widened
-// fragments of K and V take 32 more); 49 to 64 rows go as two units of two tiles.
-static int few_tiles(const PagedArgs& a, int e4m3, int max_new) {
-  const long long rows = (long long)max_new * (a.hpr / a.kvpr);
-  return rows <= 16 ? 1 : rows > 32 && rows <= 48 && !e4m3 ? 3 : 2;
-}
+// Tiles of 16 query rows per unit: one read of K and V for all of them
+static int few_tiles(const PagedArgs& a, int max_new) { return (long long)max_new * (a.hpr / a.kvpr) <= 16 ? 1 : 2; }
 
 // at most as many units as this: a sequence's last tile is not full
 static long long few_units(const PagedArgs& a, int nt) {
-  const long long grp = a.hpr / a.kvpr;
-  return std::min((a.rows * grp + 16 * nt - 1) / (16 * nt) + a.batch - 1, a.rows * grp) * a.T * a.kvpr;
+  const long long rows = (long long)a.rows * (a.hpr / a.kvpr);
+  return std::min((rows + 16 * nt - 1) / (16 * nt) + a.batch - 1, rows) * a.T * a.kvpr;
 }
 
-// 64 rows of queries and more go to the prompts' kernel; so does what would not leave the line's places 31 bits
-bool paged_few_takes(const PagedArgs& a, int e4m3, int max_new) {
+// More than 32 rows of queries go to the prompts' kernel, whose vector work per score is less (us, here with three and four
+// tiles / there: 64 / 8 heads, 24 sequences of up to 6000 keys, 24 rows 114 / 124, 40 rows 150 / 128, 64 rows 219 / 166; one of 40000
+// 44 / 59, 63 / 61, 71 / 63; in e4m3 the line would lie at 64 rows for long sequences, 123 / 132 and 46 / 58 at 40, but short ones lose
+// more: 64 sequences of 500 keys 60 / 30).  So does what would not leave the line's places 31 bits.
+bool paged_few_takes(const PagedArgs& a, int max_new) {
   const long long nb = ((long long)a.max_pages * a.page_size + 15) / 16 + FSTART * FNW;
-  return (long long)max_new * (a.hpr / a.kvpr) <= 64 && few_units(a, few_tiles(a, e4m3, max_new)) <= 0x7FFFFFFFLL / nb;
+  return (long long)max_new * (a.hpr / a.kvpr) <= 32 && few_units(a, few_tiles(a, max_new)) <= 0x7FFFFFFFLL / nb;
 }
 
-size_t paged_few_workspace_bytes(const PagedArgs& a, int e4m3, int max_new) {
-  return (size_t)FMAX_WGS * FNW * (sizeof(FewJoin) + 2 * few_tiles(a, e4m3, max_new) * 16 * FPR * sizeof(float));
+size_t paged_few_workspace_bytes(const PagedArgs& a, int max_new) {
+  return (size_t)FMAX_WGS * FNW * (sizeof(FewJoin) + 2 * few_tiles(a, max_new) * 16 * FPR * sizeof(float));
 }
 
 hipError_t launch_paged_few(const PagedArgs& a, int e4m3, int max_new, const bf16_t* q, bf16_t* out, const void* kc, const void* vc,
                             void* workspace, hipStream_t s) {
   const long long grp = a.hpr / a.kvpr, cap = (long long)a.max_pages * a.page_size;
   const long long kb = e4m3 ? 32 : 16, nb = (cap + kb - 1) / kb;
-  const int nt = few_tiles(a, e4m3, max_new);
+  const int nt = few_tiles(a, max_new);
   const long long units = few_units(a, nt);
   // A cache of so few keys that a wave does them in the time of a second kernel's launch, then one of so few that a workgroup
   // does (and the launch has one for every unit)
@@ -676,7 +676,7 @@ hipError_t launch_paged_few(const PagedArgs& a, int e4m3, int max_new, const bf1
   float* part = reinterpret_cast<float*>(joins + FMAX_WGS * FNW);
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)PHD);
   auto kernel = e4m3 ? (nt == 1 ? paged_few_kernel<true, 1> : paged_few_kernel<true, 2>)
-                     : (nt == 1 ? paged_few_kernel<false, 1> : nt == 2 ? paged_few_kernel<false, 2> : paged_few_kernel<false, 3>);
+                     : (nt == 1 ? paged_few_kernel<false, 1> : paged_few_kernel<false, 2>);
   hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(64 * FNW), 0, s, a, q, out, kc, vc, part, joins, scale_log2, least, mode, unit_joins);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || mode != FEW_LINE) return e;

@@ -176,6 +176,11 @@ def bits(t):
 FEW, MANY = 2.0 ** -13, 2.0 ** -7 + 2.0 ** -13
 
 
+def slack(c):
+    """Up to 32 (token, head of the group) rows of a sequence keep 16 bits of a probability, more of them 8."""
+    return FEW if c.desc.max_new * (c.hpr // c.kvpr) <= 32 else MANY
+
+
 def check_attn(c, got_bits, ref, size, slack):
     got = widen(got_bits)[:, :c.rows]
     own = ~np.isnan(ref)

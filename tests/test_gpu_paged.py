@@ -18,7 +18,7 @@ FEW_TOKENS = [
     (1, 8, 2, [100, 9, 0, 260], [5, 9, 0, 4], 16, False, "phrd"),            # drafts; 9 new of 9
     (1, 2, 2, [64, 200], [17, 3], 32, False, "phrd"),                        # 17 rows
     (1, 3, 1, [50, 4], [5, 4], 16, False, "phrd"),                           # 15 and 12 rows
-    (1, 16, 2, [300, 77, 50], [5, 6, 3], 16, False, "phrd"),                 # 40, 48 and 24 rows in tiles of 48
+    (1, 16, 2, [300, 77, 50], [5, 6, 3], 16, False, "phrd"),                 # 40, 48 and 24 rows
     (1, 8, 1, [1500, 30, 9], [8, 7, 1], 16, False, "phrd"),                  # 64 and 56 rows
     (1, 6, 1, [3001], [7], 64, False, "phrd"),                               # 42 rows, many workgroups inside one unit
     (1, 8, 1, [2222, 40], [4, 3], 32, True, "phrd"),                         # 32 and 24 rows
@@ -62,7 +62,7 @@ def test_attention_of_few_tokens(T, heads, kv, lens, news, page, e4m3, order):
     c = P.make(12, T, heads, kv, lens, news, page, e4m3, order, pad_rows=2)
     d = P.on_gpu(c)
     P.attend(c, d)
-    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.FEW)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
 
 
 @pytest.mark.parametrize("T,heads,kv,lens,news,page,e4m3,order", PROMPTS)
@@ -70,7 +70,23 @@ def test_attention_of_prompts(T, heads, kv, lens, news, page, e4m3, order):
     c = P.make(13, T, heads, kv, lens, news, page, e4m3, order, pad_rows=2)
     d = P.on_gpu(c)
     P.attend(c, d)
-    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.MANY)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
+
+
+@pytest.mark.parametrize("T,heads,kv,e4m3", [(8, 64, 8, True), (8, 32, 32, False), (4, 16, 8, False), (8, 64, 8, False)])
+def test_the_same_bits_every_time(T, heads, kv, e4m3):
+    """Workgroups that go through several units, waves that go through several, many joins: the same call gives the same bits, and
+    the definition's values on some rows."""
+    lens = [399, 4001, 17, 0, 1, 803, 250, 1500, 64, 333, 2048, 90, 411, 700, 37, 128, 999, 555, 16, 1201] * 3
+    c = P.make(23, T, heads, kv, lens, [int(x > 0) for x in lens], 32, e4m3)
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    first = P.bits(d.out).copy()
+    for _ in range(20):
+        d.out.fill_(-7.0)
+        P.attend(c, d)
+        assert np.array_equal(P.bits(d.out), first)
+    P.check_attn(c, first, *P.ref_attn(c), P.slack(c))
 
 
 def test_append_far_positions_and_wide_rows():
@@ -137,7 +153,7 @@ def test_what_no_query_sees_does_not_matter(e4m3, new):
             w[:, page, :, off] = fill[:, page, :, off]
     d = P.on_gpu(c)
     P.attend(c, d)
-    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.FEW if new <= 3 else P.MANY)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
 
 
 @pytest.mark.parametrize("new", [1, 3, 6, 90])
@@ -164,7 +180,7 @@ def test_infinities_that_are_seen(new, long):
     fine[0, :new, :8, 5:8] = False
     fine[0, new:, 8:] = False
     got, ref, size = got[fine], ref[fine], size[fine]
-    assert np.all(np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + (P.FEW if new * 8 <= 64 else P.MANY) * size)
+    assert np.all(np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + P.slack(c) * size)
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
@@ -182,7 +198,7 @@ def test_lists_that_are_wrong(e4m3, new):
     c.table[4, :] = c.table[5, 0]
     d = P.on_gpu(c)
     P.attend(c, d)
-    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.FEW if new <= 2 else P.MANY)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
     c.table[4, :] = -1                                   # (two tokens must not be appended to one place)
     d = P.on_gpu(c)
     P.append(c, d)
@@ -209,7 +225,7 @@ def test_without_a_list_of_rows():
     d = P.on_gpu(c)
     d.row_start = None
     P.attend(c, d)
-    P.check_attn(c, P.bits(d.out), ref, size, P.FEW)
+    P.check_attn(c, P.bits(d.out), ref, size, P.slack(c))
     P.append(c, d)
     P.check_append(c, P.bits(d.q_out), P.bits(d.k), P.bits(d.v), c.k, c.v)
 
@@ -248,4 +264,4 @@ def test_a_batch_that_grows_step_by_step(e4m3):
         k, v = P.bits(d.k).copy(), P.bits(d.v).copy()
         P.check_append(c, P.bits(d.q_out), k, v, c.k, c.v)
         c.k, c.v = k, v
-        P.check_attn(c, P.bits(d.out), *P.ref_attn(c, q=P.bits(d.q_out)), P.MANY)
+        P.check_attn(c, P.bits(d.out), *P.ref_attn(c, q=P.bits(d.q_out)), P.slack(c))
