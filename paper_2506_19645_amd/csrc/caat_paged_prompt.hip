@@ -25,6 +25,7 @@ typedef __attribute__((address_space(3))) const u32x4_t* lds_u4_t;
 typedef __attribute__((address_space(3))) const char* lds_c_t;
 typedef __attribute__((address_space(3))) short4_t* lds_s4_t;
 typedef __attribute__((address_space(4))) const int* const_i_t;
+typedef __attribute__((address_space(4))) const char* const_c_t;
 
 static constexpr int PBQ = 128;                  // query rows per workgroup (32 per wave)
 static constexpr int PBK = 64;                   // keys per block
@@ -135,33 +136,85 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
 
   // ---- pages.  `next` holds the table's entries of the 4 groups of 16 keys of block (col, in) that is copied next; a block's
   // places are made from them when its K is copied and kept for its V, one block later.
-  const const_i_t table = (const_i_t)(a.table + (long long)b * a.max_pages);
+  const const_c_t table = (const_c_t)(a.table + (long long)b * a.max_pages);
   const int gpp = a.page_size >> 4;              // groups per page
-  int next[4], ncol = blk0 * 4 / gpp, nin = blk0 * 4 - ncol * gpp;   // entries, and column and group inside the page behind them
+  const int n_pages = (int)a.n_pages;            // (the host has checked that it fits)
+  const unsigned last_col = (unsigned)(a.max_pages - 1) * 4;
+  const long long page_bytes = a.s_page * ELT, group_bytes = 16 * a.s_row * ELT;
+  const bool quad = (gpp & 3) == 0;              // a block lies inside one page
+  int next[4], nin;                              // entries; group inside its page behind them
+  unsigned ncol;                                 // and byte offset of its column
+  int pin;                                       // group inside its page of the block that is placed next (e4m3: the wave's group),
+  long long pat;                                 // and its byte offset there
+  {
+    const int col = blk0 * 4 / gpp;
+    nin = blk0 * 4 - col * gpp;
+    ncol = min((unsigned)col * 4, last_col);
+    pin = E4M3 ? (nin + wave) % gpp : nin;
+    pat = pin * group_bytes;
+  }
+  const int step = 4 % gpp;
   auto fetch = [&] {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      next[i] = table[min(ncol, a.max_pages - 1)];
-      if (++nin == gpp) {
+    if (quad) {
+      next[0] = *(const_i_t)(table + ncol);
+      if ((nin += 4) == gpp) {
         nin = 0;
-        ++ncol;
+        ncol = min(ncol + 4, last_col);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        next[i] = *(const_i_t)(table + ncol);
+        if (++nin == gpp) {
+          nin = 0;
+          ncol = min(ncol + 4, last_col);
+        }
       }
     }
   };
   struct Place {
-    long long at[4];                             // byte offsets of the groups inside a head's pages
+    long long at[E4M3 ? 1 : 4];                  // byte offsets of the groups (e4m3: of the wave's) inside a head's pages
     unsigned have;                               // groups that have a page
   };
-  int pin = nin;                                 // group inside its page of the block that is placed next
   auto place = [&] {
     Place p;
-    p.have = 0;
+    if constexpr (E4M3) {
+      int mine = next[0];
+      if (quad) {
+        p.have = (unsigned)next[0] < (unsigned)n_pages ? 15u : 0u;
+      } else {
+        p.have = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool ok = next[i] >= 0 && next[i] < a.n_pages;
-      p.at[i] = ok ? (next[i] * a.s_page + (long long)pin * 16 * a.s_row) * ELT : 0;
-      p.have |= ok ? 1u << i : 0u;
-      if (++pin == gpp) pin = 0;
+        for (int i = 0; i < 4; ++i) p.have |= (unsigned)next[i] < (unsigned)n_pages ? 1u << i : 0u;
+        mine = wave == 0 ? next[0] : wave == 1 ? next[1] : wave == 2 ? next[2] : next[3];
+      }
+      p.at[0] = (unsigned)mine < (unsigned)n_pages ? (unsigned)mine * page_bytes + pin * group_bytes : 0;
+      pin += quad ? 4 : step;
+      if (pin >= gpp) pin -= gpp;
+    } else if (quad) {
+      const bool ok = (unsigned)next[0] < (unsigned)n_pages;
+      p.have = ok ? 15u : 0u;
+      p.at[0] = ok ? (unsigned)next[0] * page_bytes + pat : 0;
+#pragma unroll
+      for (int i = 1; i < 4; ++i) p.at[i] = p.at[i - 1] + group_bytes;
+      pat += 4 * group_bytes;
+      if ((pin += 4) == gpp) {
+        pin = 0;
+        pat = 0;
+      }
+    } else {
+      p.have = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool ok = (unsigned)next[i] < (unsigned)n_pages;
+        p.at[i] = ok ? (unsigned)next[i] * page_bytes + pat : 0;
+        p.have |= ok ? 1u << i : 0u;
+        pat += group_bytes;
+        if (++pin == gpp) {
+          pin = 0;
+          pat = 0;
+        }
+      }
     }
     return p;
   };
@@ -179,18 +232,21 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
     if (E4M3) dro = (lane >> 3) * row_bytes + (lane & 7) * 16;
   }
   auto issue_rows = [&](const unsigned char* base, unsigned off, const Place& p, int blk, uint4* t) {
+    uint4* to = t + wave * 4 * PCH;
+    const int left = kv_end - key0 - blk * PBK;  // rows from here on that anybody sees
+    if (left >= PBK && p.have == 15u) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int left = p.have >> i & 1 ? kv_end - key0 - blk * PBK - i * 16 : 0;   // rows of the group that anybody sees
-      const i32x4_t rs = make_rsrc(base + p.at[i]);
-      dma16(rs, wave * 4 + (lane >> 4) < left ? off : 0x80000000u, t + (i * 16 + wave * 4) * PCH);
+      for (int i = 0; i < 4; ++i) dma16(make_rsrc(base + p.at[i]), off, to + i * 16 * PCH);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        dma16(make_rsrc(base + p.at[i]), (p.have >> i & 1) && i * 16 + wave * 4 + (lane >> 4) < left ? off : 0x80000000u, to + i * 16 * PCH);
     }
   };
   uint4* raw = smem + 4 * PTILE + (E4M3 ? wave * 256 : 0);
   auto issue_raw = [&](const unsigned char* base, const Place& p, int blk, uint4* t) {   // the wave's group
     const int left = p.have >> wave & 1 ? kv_end - key0 - blk * PBK - wave * 16 : 0;
-    const long long at = wave == 0 ? p.at[0] : wave == 1 ? p.at[1] : wave == 2 ? p.at[2] : p.at[3];
-    const i32x4_t rs = make_rsrc(base + at);
+    const i32x4_t rs = make_rsrc(base + p.at[0]);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       dma16(rs, i * 8 + (lane >> 3) < left ? dro + i * 8 * row_bytes : 0x80000000u, t + i * 64);
