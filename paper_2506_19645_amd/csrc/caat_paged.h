@@ -26,6 +26,17 @@ __device__ __forceinline__ long long lane64(long long x, int lane) {   // a lane
                      (unsigned)__builtin_amdgcn_readlane((int)x, lane));
 }
 
+// inclusive sums over the lanes of a wave
+__device__ __forceinline__ int wave_sums(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // from 1, 2, 4, 8 lanes below inside rows of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // the last lane of rows 0 and 2 to rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // lane 31 to rows 2 and 3
+  return v;
+}
+
 // The two forms of the attention: caat_paged_few.hip, caat_paged_prompt.hip
 bool paged_few_takes(const PagedArgs& a, int max_new);
 size_t paged_few_workspace_bytes(const PagedArgs& a, int max_new);

@@ -57,17 +57,6 @@ struct SeqChunk {
   int units, work;                               // of one (rank, key / value head): units and their length in the line
 };
 
-// inclusive sums over the lanes of a wave
-__device__ __forceinline__ int wave_sums(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // from 1, 2, 4, 8 lanes below inside rows of 16
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // the last lane of rows 0 and 2 to rows 1 and 3
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // lane 31 to rows 2 and 3
-  return v;
-}
-
 // How the units are dealt out.  FEW_LINE: as the head of this file says.  FEW_WAVE: whole units to waves, FEW_WG: a unit to a
 // workgroup; neither leaves anything for the second kernel.
 enum FewMode { FEW_LINE = 0, FEW_WAVE = 1, FEW_WG = 2 };

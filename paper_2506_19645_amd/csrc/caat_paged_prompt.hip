@@ -35,11 +35,25 @@ static constexpr int PRAW = 4 * 256;             // chunks of the waves' e4m3 bu
 static constexpr int PPR = PHD + 4;              // floats of a partial row: 128 sums, maximum, denominator, 2 unused
 static constexpr int PWGS = 512;                 // workgroups that run at a time
 
-// A tile whose keys are dealt to several workgroups: what the first of them says to the kernel that joins their results
+// Few tiles (at most PLINE, of all heads) do not fill the chip, or fill it unevenly: then the tiles of all sequences stand in one
+// line, each as long as its blocks and PSTART more (its start and its results' way), and every workgroup takes an equal stretch.
+// Places count sixteenths of a block; a tile's length is taken as linear in its number, nb0 blocks the first to nb0 + slope / 16 *
+// number, which is what causality makes it up to roundings.
+static constexpr int PLINE = 384;
+static constexpr int PSTART = 3 * 16;
+static constexpr int PLEAST = 8 * 16;            // shortest stretch
+
+// What the workgroup in which a tile's blocks begin says about it to the kernel that joins its parts
 struct PromptJoin {
   int rows;                                      // 0: nothing to join
   int rank, kvh, first, row0;
-  int unused[3];
+  int begin, end, per;                           // places of the tile's blocks, length of a stretch
+};
+
+struct PromptSeq {                               // a sequence's tiles (of one rank and key / value head)
+  int first, n, len, tiles, nb0, slope;
+  __device__ __forceinline__ int length(int t) const { return PSTART + nb0 * 16 + slope * t; }
+  __device__ __forceinline__ int before(int t) const { return t * (PSTART + nb0 * 16) + slope * (t * (t - 1) / 2); }
 };
 
 __device__ __forceinline__ int pk_swz(int row, int c) { return c ^ (row & 15); }
@@ -51,10 +65,12 @@ __device__ __forceinline__ float pmax3(float a, float b, float c) {
   return d;
 }
 
-template <bool E4M3>
+// LINE: the workgroup takes a stretch of the line (line_room: tiles that joins has room for), otherwise one tile
+template <bool E4M3, bool LINE>
 __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a, const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
                                                               const void* __restrict__ kc, const void* __restrict__ vc,
-                                                              float* __restrict__ part, PromptJoin* __restrict__ joins, float scale_log2) {
+                                                              float* __restrict__ part, PromptJoin* __restrict__ joins, float scale_log2,
+                                                              int line_room) {
   constexpr int ELT = E4M3 ? 1 : 2;
   __shared__ uint4 smem[4 * PTILE + (E4M3 ? PRAW : 0)];   // K slots 0 and 1, V slots 0 and 1, 16 KB each; e4m3 buffers
   const int tid = threadIdx.x, lane = tid & 63;
@@ -62,49 +78,119 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
   const int frow = lane & 31, hf = lane >> 5;
   const int grp = a.hpr / a.kvpr, heads = a.T * a.kvpr;
 
-  // ---- which rows: the launch runs through the tiles of all sequences, heads innermost (a head's tiles run on one XCD, close
-  // in time, where the number of heads is a multiple of 8), a sequence's last tile, which sees most keys, first
-  const int h = blockIdx.x % heads;
-  int tile = blockIdx.x / heads, b = -1, first = 0, n = 0;
-  for (int at = 0; at < a.batch && b < 0; at += 64) {
-    int f = 0, m = 0;
-    if (at + lane < a.batch) m = seq_rows(a, at + lane, f);
-    const int mine = (int)(((long long)m * grp + PBQ - 1) / PBQ);
-    int incl = mine;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int up = __shfl_up(incl, off, 64);
-      if (lane >= off) incl += up;
-    }
-    const unsigned long long over = __ballot(incl > tile);
-    if (over) {
-      const int l = __builtin_ctzll(over);
-      tile -= __builtin_amdgcn_readlane(incl - mine, l);
-      first = __builtin_amdgcn_readlane(f, l);
-      n = __builtin_amdgcn_readlane(m, l);
-      tile = __builtin_amdgcn_readlane(mine, l) - 1 - tile;
-      b = at + l;
-    } else {
-      tile -= __builtin_amdgcn_readlane(incl, 63);
-    }
-  }
-  const int splits = gridDim.y, split = blockIdx.y;
-  if (b < 0) {                                   // fewer tiles than the launch has room for
-    if (splits > 1 && split == 0 && tid == 0) joins[blockIdx.x].rows = 0;
-    return;
-  }
-  const int rank = h / a.kvpr, kvh = h - rank * a.kvpr;
-  const int len = max(uni(a.lens[b]), 0);
   const int cap = a.max_pages * a.page_size;
+  // blocks of keys that a tile's rows see; a token t of n sees those below len - n + t + 1
+  auto tile_end = [&](int n, int len, int t) {   // may be 0 or less
+    const int last_token = min(n - 1, (int)(((long long)t * PBQ + PBQ - 1) / grp));
+    return min(min(len, cap), len - n + last_token + 1);
+  };
+  auto load_seq = [&](int b) {
+    PromptSeq q;
+    q.first = q.n = q.len = q.tiles = q.nb0 = q.slope = 0;
+    if (b < a.batch) {
+      q.n = seq_rows(a, b, q.first);
+      q.len = max(a.lens[b], 0);
+      q.tiles = (int)(((long long)q.n * grp + PBQ - 1) / PBQ);
+      if (LINE && q.tiles > 0) {
+        q.nb0 = max(1, (tile_end(q.n, q.len, 0) + PBK - 1) / PBK);
+        const int nbl = max(q.nb0, (tile_end(q.n, q.len, q.tiles - 1) + PBK - 1) / PBK);
+        q.slope = 16 * (nbl - q.nb0) / max(q.tiles - 1, 1);
+      }
+    }
+    return q;
+  };
+  auto pick = [](const PromptSeq& q, int l) {
+    return PromptSeq{__builtin_amdgcn_readlane(q.first, l), __builtin_amdgcn_readlane(q.n, l), __builtin_amdgcn_readlane(q.len, l),
+                     __builtin_amdgcn_readlane(q.tiles, l), __builtin_amdgcn_readlane(q.nb0, l), __builtin_amdgcn_readlane(q.slope, l)};
+  };
+
+  // ---- which rows.  Without a line: one tile.  The launch runs through the tiles of all sequences, heads innermost
+  // (a head's tiles run on one XCD, close in time, where the number of heads is a multiple of 8), a sequence's last tile,
+  // which sees most keys, first.
+  int b = -1, h = blockIdx.x % heads, tile = blockIdx.x / heads, base = 0, unit0 = 0, x = 0, x1 = 1, per = 1;
+  PromptSeq sq = {};
+  if constexpr (!LINE) {
+    for (int at = 0; at < a.batch && b < 0; at += 64) {
+      const PromptSeq c = load_seq(at + lane);
+      const int incl = wave_sums(c.tiles);
+      const unsigned long long over = __ballot(incl > tile);
+      if (over) {
+        const int l = __builtin_ctzll(over);
+        sq = pick(c, l);
+        tile = __builtin_amdgcn_readlane(incl, l) - 1 - tile;
+        b = at + l;
+      } else {
+        tile -= __builtin_amdgcn_readlane(incl, 63);
+      }
+    }
+    if (b < 0) return;                           // fewer tiles than the launch has room for
+  } else {
+    // neighbours in the line share keys: an XCD takes workgroups that stand together in it
+    const int taker = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+    PromptSeq c = load_seq(lane);
+    int own = c.before(c.tiles), incl = wave_sums(own), uincl = wave_sums(c.tiles);
+    int total = __builtin_amdgcn_readlane(incl, 63), units = __builtin_amdgcn_readlane(uincl, 63);
+    for (int at = 64; at < a.batch; at += 64) {
+      const PromptSeq d = load_seq(at + lane);
+      total += __builtin_amdgcn_readlane(wave_sums(d.before(d.tiles)), 63);
+      units += __builtin_amdgcn_readlane(wave_sums(d.tiles), 63);
+    }
+    total *= heads;                              // (the host has checked that this is below 2^31)
+    units *= heads;
+    for (int i = units + taker * 256 + tid; i < line_room; i += gridDim.x * 256) joins[i].rows = 0;
+    per = max((int)((unsigned)(total + gridDim.x - 1) / gridDim.x), PLEAST);
+    x = (int)min((long long)taker * per, (long long)total);
+    x1 = min(total - x, per) + x;
+    if (x >= x1) return;
+    for (int at = 0; at < a.batch; at += 64) {
+      if (at > 0) {
+        c = load_seq(at + lane);
+        own = c.before(c.tiles);
+        incl = wave_sums(own);
+        uincl = wave_sums(c.tiles);
+      }
+      const unsigned long long over = __ballot(base + incl * heads > x);
+      if (over) {
+        const int l = __builtin_ctzll(over);
+        sq = pick(c, l);
+        base += __builtin_amdgcn_readlane(incl - own, l) * heads;
+        unit0 += __builtin_amdgcn_readlane(uincl - c.tiles, l) * heads;
+        b = at + l;
+        break;
+      }
+      base += __builtin_amdgcn_readlane(incl, 63) * heads;
+      unit0 += __builtin_amdgcn_readlane(uincl, 63) * heads;
+    }
+    if (b < 0) return;                           // (a list that gives rows twice and is longer than 31 bits)
+    const int one = sq.before(sq.tiles);
+    h = (int)((unsigned)(x - base) / (unsigned)one);
+    const int r = x - base - h * one;
+    for (tile = 0; tile + 64 <= sq.tiles && sq.before(tile + 64) <= r; tile += 64) {}
+    tile += __popcll(__ballot(tile + lane < sq.tiles && sq.before(tile + lane) <= r)) - 1;
+  }
+  const float scale0 = scale_log2;
+
+  for (bool more = false;; more = true) {        // the tiles of the stretch
+  const int n = sq.n, first = sq.first, len = sq.len;
+  const int rank = h / a.kvpr, kvh = h - rank * a.kvpr;
   const int keys = min(len, cap);
-  // keys that token t sees: below len - n + t + 1
   const int row0 = tile * PBQ;
-  const int last_token = min(n - 1, (row0 + PBQ - 1) / grp);
-  const int kv_end = (int)min((long long)keys, (long long)len - n + last_token + 1);   // may be 0 or less
+  const int kv_end = tile_end(n, len, tile);     // may be 0 or less
   const int all_blk = max(0, (kv_end + PBK - 1) / PBK);
-  const int blk0 = (int)((long long)all_blk * split / splits);   // this workgroup's share: blocks blk0 .. blk0 + nblk - 1
-  const int nblk = (int)((long long)all_blk * (split + 1) / splits) - blk0;
+  // its blocks that are this workgroup's: blk0 .. blk0 + nblk - 1
+  int begin = 0, end = 1, blk0 = 0, blk1 = all_blk;
+  if (LINE) {
+    end = base + h * sq.before(sq.tiles) + sq.before(tile + 1);
+    const int length = sq.length(tile) - PSTART;
+    begin = end - length;
+    if (x1 <= begin) break;                      // the stretch ends in front of the first one
+    blk0 = (int)((long long)all_blk * (max(x, begin) - begin) / length);
+    blk1 = (int)((long long)all_blk * (min(x1, end) - begin) / length);
+  }
+  const bool begins = x <= begin, all_here = begins && x1 >= end;
+  const int nblk = blk1 - blk0;
   const int key0 = blk0 * PBK;
+  if (LINE && more) __syncthreads();                     // everyone is done with the last tile's blocks
 
   // ---- Q fragments: B operand of S^T = K q^T: lane (row frow, k-half hf) holds q[16 ks + 8 hf .. + 7]
   const int qr = row0 + wave * 32 + frow;
@@ -114,18 +200,10 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
   const int lim = row_ok ? (int)min((long long)len - n + token + 1, (long long)keys) : kv_end;
   const int wave_lim = uni((int)min((long long)len - n + (row0 + wave * 32) / grp + 1, (long long)keys));   // of the wave's first row
   bf16x8_t qf[PHD / 16];
-  {
-    uint4 w[PHD / 16];
-    const bf16_t* src = q + (row_ok ? qrow * a.ld_q + head * PHD : 0) + hf * 8;   // rows of nobody: any row, not stored
+  const bf16_t* src = q + (row_ok ? qrow * a.ld_q + head * PHD : 0) + hf * 8;   // rows of nobody: any row, not stored
 #pragma unroll
-    for (int ks = 0; ks < PHD / 16; ++ks) w[ks] = *reinterpret_cast<const uint4*>(src + ks * 16);
-#pragma unroll
-    for (int ks = 0; ks < PHD / 16; ++ks) {
-      asm volatile("" : "+v"(w[ks].x), "+v"(w[ks].y), "+v"(w[ks].z), "+v"(w[ks].w));   // the wait for q stands in front of the loop
-      qf[ks] = __builtin_bit_cast(bf16x8_t, w[ks]);
-    }
-  }
-  if (E4M3 && a.k_scale) scale_log2 *= a.k_scale[h];
+  for (int ks = 0; ks < PHD / 16; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(src + ks * 16);
+  scale_log2 = E4M3 && a.k_scale ? scale0 * a.k_scale[h] : scale0;
 
   f32x16_t oacc[PHD / 32];
 #pragma unroll
@@ -464,6 +542,8 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
       have_next = pk.have;
     }
 #pragma unroll
+    for (int ks = 0; ks < PHD / 16; ++ks) asm volatile("" : "+v"(qf[ks]));   // the compiler's wait for q stands in front of the loop
+#pragma unroll
     for (int j = 0; j < PBK / 32; ++j)
 #pragma unroll
       for (int ks = 0; ks < PHD / 16; ++ks) {
@@ -485,10 +565,15 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
 
   // ---- normalise and store: lane holds out[row][32 dt + 8 (r / 4) + 4 hf + r % 4]
   l_run += __shfl_xor(l_run, 32, 64);
-  if (splits > 1) {
-    if (split == 0 && tid == 0) joins[blockIdx.x] = PromptJoin{min(PBQ, n * grp - row0), rank, kvh, first, row0, {0, 0, 0}};
+  if (LINE && begins && tid == 0) {
+    PromptJoin* j = joins + unit0 + h * sq.tiles + tile;
+    if (unit0 + h * sq.tiles + tile < line_room)
+      *j = PromptJoin{all_here ? 0 : min(PBQ, n * grp - row0), rank, kvh, first, row0, begin, end, per};
+  }
+  if (LINE && !all_here) {
+    const int taker = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
     if (row_ok) {
-      float* o = part + (((long long)blockIdx.x * splits + split) * PBQ + wave * 32 + frow) * PPR;
+      float* o = part + ((2LL * taker + (begins ? 1 : 0)) * PBQ + wave * 32 + frow) * PPR;
 #pragma unroll
       for (int dt = 0; dt < PHD / 32; ++dt)
 #pragma unroll
@@ -497,9 +582,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
               make_float4(oacc[dt][k * 4], oacc[dt][k * 4 + 1], oacc[dt][k * 4 + 2], oacc[dt][k * 4 + 3]);
       if (hf == 0) *reinterpret_cast<float2*>(o + PHD) = make_float2(m_run * scale_log2, l_run);
     }
-    return;
-  }
-  if (row_ok) {
+  } else if (row_ok) {
     const float inv = l_run == 0.0f ? 0.0f : (E4M3 && a.v_scale ? a.v_scale[h] : 1.0f) / l_run;
     bf16_t* o = out + (qrow * a.hpr + head) * PHD;
 #pragma unroll
@@ -512,26 +595,47 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
         *reinterpret_cast<uint2*>(o + dt * 32 + k * 8 + hf * 4) = w;
       }
   }
+  // ---- the next tile
+  if (!LINE || x1 <= end) break;
+  x = end;
+  if (++tile == sq.tiles) {
+    tile = 0;
+    if (++h == heads) {
+      h = 0;
+      base += heads * sq.before(sq.tiles);
+      unit0 += heads * sq.tiles;
+      do {
+        if (++b >= a.batch) return;
+        sq = load_seq(b);                        // (all lanes the same)
+        sq = pick(sq, 0);
+      } while (sq.tiles == 0);
+    }
+  }
+  }
 }
 
-// Joins the shares of a tile's keys, in their order: 32 threads per row, 4 channels each.
+// Joins the parts of a tile, in the order of the keys: 32 threads, 4 channels each, for a row and every SUBS-th part of it.
+template <int SUBS>
 __global__ __launch_bounds__(256) void paged_prompt_join_kernel(const PagedArgs a, const float* __restrict__ part,
-                                                                const PromptJoin* __restrict__ joins, bf16_t* __restrict__ out, int splits) {
+                                                                const PromptJoin* __restrict__ joins, bf16_t* __restrict__ out) {
+  __shared__ float4 s_num[SUBS > 1 ? 256 : 1];
+  __shared__ float2 s_ml[SUBS];
   const PromptJoin j = joins[blockIdx.x];
-  const int r = blockIdx.y * 8 + (threadIdx.x >> 5), c = (threadIdx.x & 31) * 4;
-  if (r >= j.rows) return;
-  const float* p = part + ((long long)blockIdx.x * splits * PBQ + r) * PPR;
+  const int sub = (threadIdx.x >> 5) % SUBS, r = blockIdx.y * (8 / SUBS) + (threadIdx.x >> 5) / SUBS, c = (threadIdx.x & 31) * 4;
+  if (r >= j.rows) return;                       // (SUBS 8: the whole workgroup)
+  const int w0 = j.begin / j.per, parts = (j.end - 1) / j.per + 1 - w0;
   float M = -INFINITY, den = 0.0f;
   float4 num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int s0 = 0; s0 < splits; s0 += 4) {
+  for (int p0 = sub; p0 < parts; p0 += 4 * SUBS) {
     float2 ml[4];
     float4 v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float* q = p + (long long)min(s0 + i, splits - 1) * PBQ * PPR;
+      const int k = min(p0 + i * SUBS, parts - 1);
+      const float* q = part + ((2LL * (w0 + k) + (k == 0 ? 1 : 0)) * PBQ + r) * PPR;   // the first one's lies behind that of the tile before
       ml[i] = *reinterpret_cast<const float2*>(q + PHD);
       v[i] = *reinterpret_cast<const float4*>(q + c);
-      if (s0 + i >= splits) ml[i].x = -INFINITY;
+      if (p0 + i * SUBS >= parts) ml[i].x = -INFINITY;
     }
     const float m_new = fmaxf(fmaxf(M, ml[0].x), fmaxf(fmaxf(ml[1].x, ml[2].x), ml[3].x)), mb = m_new == -INFINITY ? 0.0f : m_new;
     const float alpha = __builtin_amdgcn_exp2f(M - mb);
@@ -540,10 +644,29 @@ __global__ __launch_bounds__(256) void paged_prompt_join_kernel(const PagedArgs 
     num = make_float4(num.x * alpha, num.y * alpha, num.z * alpha, num.w * alpha);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (s0 + i >= splits) break;
+      if (p0 + i * SUBS >= parts) break;
       const float f = __builtin_amdgcn_exp2f(ml[i].x - mb);
       den += ml[i].y * f;
       num = make_float4(num.x + v[i].x * f, num.y + v[i].y * f, num.z + v[i].z * f, num.w + v[i].w * f);
+    }
+  }
+  if constexpr (SUBS > 1) {
+    s_num[threadIdx.x] = num;
+    if ((threadIdx.x & 31) == 0) s_ml[sub] = make_float2(M, den);
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    M = s_ml[0].x;
+#pragma unroll
+    for (int k = 1; k < SUBS; ++k) M = fmaxf(M, s_ml[k].x);
+    const float mb = M == -INFINITY ? 0.0f : M;
+    den = 0.0f;
+    num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int k = 0; k < SUBS; ++k) {
+      const float f = __builtin_amdgcn_exp2f(s_ml[k].x - mb);
+      const float4 v = s_num[k * 32 + threadIdx.x];
+      den += s_ml[k].y * f;
+      num = make_float4(num.x + v.x * f, num.y + v.y * f, num.z + v.z * f, num.w + v.w * f);
     }
   }
   const int grp = a.hpr / a.kvpr, qr = j.row0 + r, token = qr / grp, h = j.kvh * grp + (qr - token * grp);
@@ -558,40 +681,27 @@ static long long prompt_tiles(const PagedArgs& a) {
   return std::min((rows + PBQ - 1) / PBQ + a.batch - 1, rows) * a.T * a.kvpr;
 }
 
-// Workgroups per tile.  Few tiles over many keys leave compute units idle; a share of the keys costs about 5 blocks' time more (its
-// start, its results' way through memory).  The host knows the table's width, not the lengths.
-static int prompt_splits(const PagedArgs& a) {
-  const long long tiles = prompt_tiles(a), nb = ((long long)a.max_pages * a.page_size + PBK - 1) / PBK;
-  int best = 1;
-  double cost = 0.0;
-  for (int s = 1; s <= 64 && (s == 1 || (tiles * s <= 2 * PWGS && nb / s >= 8)); ++s) {
-    const double c = (double)((tiles * s + PWGS - 1) / PWGS) * ((double)((nb + s - 1) / s) + (s > 1 ? 5.0 : 0.0));
-    if (s == 1 || c < cost) {
-      cost = c;
-      best = s;
-    }
-  }
-  return best;
-}
-
 size_t paged_prompt_workspace_bytes(const PagedArgs& a) {
-  const long long tiles = prompt_tiles(a);       // (whatever the table's width: the largest number of shares)
-  const long long shares = tiles > PWGS ? 0 : std::min<long long>(64, 2 * PWGS / tiles);
-  return shares < 2 ? 0 : (size_t)tiles * (sizeof(PromptJoin) + shares * PBQ * PPR * sizeof(float));
+  return prompt_tiles(a) > PLINE ? 0 : PLINE * sizeof(PromptJoin) + 2 * PWGS * (size_t)(PBQ * PPR) * sizeof(float);
 }
 
 hipError_t launch_paged_prompt(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, void* workspace,
                                hipStream_t s) {
-  const long long tiles = prompt_tiles(a);
-  const int splits = prompt_splits(a);
+  const long long tiles = prompt_tiles(a), most = ((long long)a.max_pages * a.page_size / PBK + 2) * 16 + PSTART;   // of a tile
+  const int line_room = tiles <= PLINE && most >= 24 * 16 && most <= 0x7FFFFFFFLL / tiles ? (int)tiles : 0;
   PromptJoin* joins = reinterpret_cast<PromptJoin*>(workspace);
-  float* part = reinterpret_cast<float*>(joins + tiles);
+  float* part = reinterpret_cast<float*>(joins + PLINE);
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)PHD);
-  auto kernel = e4m3 ? paged_prompt_kernel<true> : paged_prompt_kernel<false>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)splits), dim3(256), 0, s, a, q, out, kc, vc, part, joins, scale_log2);
+  auto kernel = e4m3 ? (line_room ? paged_prompt_kernel<true, true> : paged_prompt_kernel<true, false>)
+                     : (line_room ? paged_prompt_kernel<false, true> : paged_prompt_kernel<false, false>);
+  const long long wgs = line_room ? std::min<long long>(PWGS, (most * tiles / PLEAST + 8) / 8 * 8) : tiles;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), 0, s, a, q, out, kc, vc, part, joins, scale_log2, line_room);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || splits == 1) return e;
-  hipLaunchKernelGGL(paged_prompt_join_kernel, dim3((unsigned)tiles, PBQ / 8), dim3(256), 0, s, a, part, joins, out, splits);
+  if (e != hipSuccess || !line_room) return e;
+  if (tiles <= PWGS / 8)                         // many parts of a tile
+    hipLaunchKernelGGL(paged_prompt_join_kernel<8>, dim3((unsigned)tiles, PBQ), dim3(256), 0, s, a, part, joins, out);
+  else
+    hipLaunchKernelGGL(paged_prompt_join_kernel<1>, dim3((unsigned)tiles, PBQ / 8), dim3(256), 0, s, a, part, joins, out);
   return hipGetLastError();
 }
 
