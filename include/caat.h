@@ -336,6 +336,18 @@ int caat_paged_attn(const caat_paged_desc* d, const void* q, void* out, const in
                     const int* page_table, const void* k_cache, const void* v_cache, const float* k_scale,
                     const float* v_scale, void* workspace, size_t ws_bytes, void* hip_stream);
 
+/*
+ * The decoder layer of CAAT_ATTN_DECODE (RMSNorm, q/k/v projections, attention, o_proj, the partial channel-reduce, SwiGLU MLP)
+ * over a paged cache, for any number of new tokens per sequence: decode steps, prompts and chunks of them, drafts, mixed in
+ * one batch.  d: kind CAAT_ATTN_DECODE with tokens = batch = pages->rows and seq = 1 (kv_len and kv_cap are not read); T, n_heads,
+ * n_kv_heads, head_dim and rope_base as in pages, whose ld_q and ld_qkv are 0.  weights, r, r_out as in caat_block_fwd.  r_out
+ * of rows that belong to no sequence is written too and means nothing.
+ */
+size_t caat_paged_layer_workspace_bytes(const caat_desc* d, const caat_paged_desc* pages);
+int caat_paged_layer_fwd(const caat_desc* d, const caat_paged_desc* pages, const void* const* weights, const void* r, void* r_out,
+                         const int* row_start, const int* lens, const int* page_table, void* k_cache, void* v_cache,
+                         const float* k_scale, const float* v_scale, void* workspace, size_t ws_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

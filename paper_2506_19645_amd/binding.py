@@ -55,7 +55,8 @@ class caat_ws_layout(C.Structure):
 EXPORTS = ["caat_shared_channels", "caat_status_string", "caat_workspace_bytes", "caat_workspace_layout",
            "caat_partial_sync", "caat_norm_fwd", "caat_partial_sync_norm_fwd", "caat_norm_bwd_workspace_bytes",
            "caat_norm_bwd", "caat_norm_bwd_static", "caat_gemm_bf16", "caat_block_fwd", "caat_block_bwd",
-           "caat_paged_append", "caat_paged_attn_workspace_bytes", "caat_paged_attn"]
+           "caat_paged_append", "caat_paged_attn_workspace_bytes", "caat_paged_attn", "caat_paged_layer_workspace_bytes",
+           "caat_paged_layer_fwd"]
 TOOL_EXPORTS = ["caat_profile_enable", "caat_profile_reset", "caat_profile_count", "caat_profile_get", "caat_hbm_probe",
                 "caat_gemm_route", "caat_gemm_pair_route",
                 "caat_gemm_shared_pair_route"]
@@ -105,6 +106,10 @@ def lib() -> C.CDLL:
         L.caat_paged_attn_workspace_bytes.restype = sz
         L.caat_paged_attn.argtypes = [pd, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.caat_paged_attn.restype = i
+        L.caat_paged_layer_workspace_bytes.argtypes = [C.POINTER(caat_desc), pd]
+        L.caat_paged_layer_workspace_bytes.restype = sz
+        L.caat_paged_layer_fwd.argtypes = [C.POINTER(caat_desc), pd, C.POINTER(vp), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.caat_paged_layer_fwd.restype = i
         L.caat_profile_enable.argtypes = [i]
         L.caat_profile_enable.restype = i
         L.caat_profile_reset.argtypes = []
@@ -318,6 +323,21 @@ def paged_attn(desc: caat_paged_desc, q, out, row_start, lens, page_table, k_cac
                                _stream(stream))
     if check:
         _check(st, "caat_paged_attn")
+    return st
+
+
+def paged_layer_workspace_bytes(desc: caat_desc, pages: caat_paged_desc) -> int:
+    return lib().caat_paged_layer_workspace_bytes(C.byref(desc), C.byref(pages))
+
+
+def paged_layer_fwd(desc: caat_desc, pages: caat_paged_desc, weights: Sequence, r, r_out, row_start, lens, page_table, k_cache,
+                    v_cache, workspace, k_scale=None, v_scale=None, stream=None, check: bool = True) -> int:
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    st = lib().caat_paged_layer_fwd(C.byref(desc), C.byref(pages), _ptr_array(weights), _ptr(r), _ptr(r_out), _ptr(row_start),
+                                    _ptr(lens), _ptr(page_table), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
+                                    _ptr(workspace), ws_bytes, _stream(stream))
+    if check:
+        _check(st, "caat_paged_layer_fwd")
     return st
 
 

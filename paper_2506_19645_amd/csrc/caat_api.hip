@@ -431,106 +431,7 @@ int attn_block_bwd(const caat_desc* d, const caat_ws_layout& L, const void* cons
   return hip_status(e);
 }
 
-// One Llama-style decoder layer at inference (which uses the partial channel-reduce too, Sec. 3.2), either for one
-// new token per sequence over a KV cache (decode) or for a whole prompt that fills the cache (prefill, the
-// time-to-first-token workload of Sec. 5.2): RMSNorm -> q,k,v -> RoPE -> store k,v in the cache -> attention
-// (streaming over kv_len+1 keys / causal flash attention over the prompt) -> o_proj -> PCR + residual -> RMSNorm ->
-// SwiGLU MLP -> PCR + residual.
-int layer_fwd(const caat_desc* d, const caat_ws_layout& L, const void* const* weights, const void* r, void* r_out,
-              void* kv_k, void* kv_v, void* workspace, size_t ws_bytes, void* hip_stream) {
-  const bool prefill = d->kind == CAAT_LAYER_PREFILL;
-  if (!weights || !r || !r_out || !kv_k || !kv_v || !workspace) return CAAT_EINVAL;
-  const void* g_attn = weights[0]; const void* wqkv = weights[1]; const void* wo = weights[2];
-  const void* g_mlp = weights[3]; const void* wgu = weights[4]; const void* wb = weights[5];
-  if (!g_attn || !wqkv || !wo || !g_mlp || !wgu || !wb) return CAAT_EINVAL;
-  if (!(d->rope_base > 0.0f)) return CAAT_EINVAL;
-  if (d->norm != CAAT_RMSNORM || d->head_dim != 128) return CAAT_EUNSUPPORTED;
-  if (prefill) {
-    if (d->kv_len != 0 || d->kv_cap < d->seq) return CAAT_ESHAPE;     // the prompt starts an empty cache
-  } else {
-    if (d->seq != 1 || d->kv_len < 0 || d->kv_cap <= d->kv_len) return CAAT_ESHAPE;
-  }
-  if (d->kv_cap * 256 >= 0x7FFFFFFFLL) return CAAT_ESHAPE;
-  if (misaligned(g_attn) || misaligned(wqkv) || misaligned(wo) || misaligned(g_mlp) || misaligned(wgu) || misaligned(wb) ||
-      misaligned(r) || misaligned(r_out) || misaligned(kv_k) || misaligned(kv_v) || misaligned(workspace))
-    return CAAT_EALIGN;
-  if (ws_bytes < (L.bytes_scratch ? L.off_scratch : L.total_bytes)) return CAAT_EWORKSPACE;   // see layer_scratch
-  if (d->tokens == 0) return CAAT_OK;
-  hipStream_t s = (hipStream_t)hip_stream;
-  char* ws = (char*)workspace;
-  const long long T = d->T, n = d->tokens, h = d->h, hpr = d->n_heads / d->T, hd = hpr * d->head_dim, fr = d->ffn / d->T;
-  const long long kvpr = kv_heads_of(d) / d->T, qw = qkv_width(d);
-  bf16_t* X1 = (bf16_t*)(ws + L.off_X1);
-  bf16_t* QKV = (bf16_t*)(ws + L.off_Q);
-  bf16_t* H = (bf16_t*)(ws + L.off_H);
-  bf16_t* R1 = (bf16_t*)(ws + L.off_R1);
-  bf16_t* X2 = (bf16_t*)(ws + L.off_X2);
-  bf16_t* P = (bf16_t*)(ws + L.off_P);
-  bf16_t* Y = (bf16_t*)(ws + L.off_Y);
-  float* rstd = (float*)(ws + L.off_rstd);
-  void* scratch = L.bytes_scratch ? ws + L.off_scratch : nullptr;
-  const size_t scratch_bytes = scratch ? std::min(L.bytes_scratch, ws_bytes - L.off_scratch) : 0;
-  hipError_t e;
-  GemmParams q;
-#define CAAT_STEP(name, call) { ProfScope ps(s, name); e = (call); } if (e != hipSuccess) return CAAT_EHIP;
-  CAAT_STEP("norm_fwd", launch_norm_fwd((const bf16_t*)r, (const bf16_t*)g_attn, nullptr, X1, nullptr, rstd, CAAT_RMSNORM, (int)T,
-                                        n, (int)h, d->eps, s, dedup_hs(d)))
-  std::memset(&q, 0, sizeof(q));
-  q.a = X1; q.lda = h; q.stride_a = n * h;
-  q.b = (const bf16_t*)wqkv; q.ldb = h; q.stride_b = qw * h;
-  q.c = QKV; q.ldc = qw; q.stride_c = n * qw;
-  q.G = (int)T; q.M = (int)n; q.N = (int)qw; q.K = (int)h;
-  q.rope = {(int)d->seq, (int)hpr * 128, (int)kvpr * 128, (int)d->batch, log2f(d->rope_base), (bf16_t*)kv_k, (bf16_t*)kv_v, d->kv_cap};
-  const bool rotate = prefill && rope_in_gemm(q);
-  CAAT_STEP("gemm_nt_qkv", launch_gemm(q, 0, rotate ? EPI_ROPE : EPI_PLAIN, s))
-  if (prefill) {
-    if (!rotate) {
-      CAAT_STEP("rope_kv_append", launch_rope_append(QKV, (bf16_t*)kv_k, (bf16_t*)kv_v, T * d->batch, d->seq, (int)hpr, (int)kvpr,
-                                                     d->head_dim, d->rope_base, d->kv_cap, d->kv_len, s))
-    }
-    CAAT_STEP("flash_attn_fwd", launch_flash_fwd(QKV, H, nullptr, T * d->batch, d->seq, (int)hpr, (int)kvpr, d->head_dim, s))
-  } else {
-    // decode: the attention kernel rotates q and the new k itself, appends k, v to the caches and attends to
-    // kv_len cached keys plus the new one
-    CAAT_STEP("decode_attn", launch_decode_attn(QKV, (bf16_t*)kv_k, (bf16_t*)kv_v, H, T * n, (int)hpr, (int)kvpr,
-                                                d->head_dim, d->kv_cap, d->kv_len + 1, d->rope_base,
-                                                scratch, scratch_bytes, s))
-  }
-  // the reduce after o_proj and the RMSNorm in front of the MLP run as one launch where the fused kernel takes the
-  // shape: for decode-sized batches both are start-up latency, for prompts the fused kernel does not read the
-  // reduced shared channels back from memory (measured 1.28 ms instead of 0.61 + 0.78 ms on 16 prompts of 2048)
-  const bool fuse_mid = fuse_reduce_norm(d), spread = spread_reduce_norm(d, scratch_bytes);
-  {
-    const int st = rowpar_pcr(d, H, hd, (const bf16_t*)wo, (const bf16_t*)r, spread ? (bf16_t*)scratch : R1, scratch,
-                              scratch_bytes, s, fuse_mid);
-    if (st != CAAT_OK) return st;
-  }
-  if (spread) {
-    CAAT_STEP("partial_sync_norm_fwd", launch_sync_norm_rank((const bf16_t*)scratch, (const bf16_t*)r, (const bf16_t*)g_mlp, R1, X2,
-                                                             rstd, (int)T, n, (int)h, d->hs, d->eps, s))
-  } else if (fuse_mid) {
-    CAAT_STEP("partial_sync_norm_fwd", launch_sync_norm(R1, (const bf16_t*)r, (const bf16_t*)g_mlp, nullptr, X2, nullptr, rstd,
-                                                        CAAT_RMSNORM, (int)T, n, (int)h, d->hs, d->eps, s))
-  } else {
-    CAAT_STEP("norm_fwd", launch_norm_fwd(R1, (const bf16_t*)g_mlp, nullptr, X2, nullptr, rstd, CAAT_RMSNORM, (int)T, n, (int)h,
-                                          d->eps, s, dedup_hs(d)))
-  }
-  std::memset(&q, 0, sizeof(q));
-  q.a = X2; q.lda = h; q.stride_a = n * h;
-  q.b = (const bf16_t*)wgu; q.ldb = h; q.stride_b = 2 * fr * h;
-  q.c = P; q.ldc = 2 * fr; q.stride_c = n * 2 * fr;
-  q.c2 = Y; q.ldc2 = fr; q.stride_c2 = n * fr;
-  q.G = (int)T; q.M = (int)n; q.N = (int)fr; q.K = (int)h; q.half = (int)fr;
-  CAAT_STEP("gemm_nt_swiglu_fwd", launch_gemm(q, 0, EPI_SWIGLU_FWD, s))
-  {
-    const int st = rowpar_pcr(d, Y, fr, (const bf16_t*)wb, R1, (bf16_t*)r_out, scratch, scratch_bytes, s);
-    if (st != CAAT_OK) return st;
-  }
-#undef CAAT_STEP
-  return CAAT_OK;
-}
-
-// ---- paged cache: the checks that both of its calls share, and the kernels' arguments
+// ---- paged cache: the checks that its calls share, and the kernels' arguments
 int paged_args(const caat_paged_desc* d, const int* row_start, const int* lens, const int* page_table, const float* k_scale,
                const float* v_scale, PagedArgs* a) {
   if (!d || d->T < 1 || d->batch < 1 || d->rows < 0 || d->n_pages < 0 || d->max_new < 1) return CAAT_EINVAL;
@@ -573,6 +474,121 @@ inline bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) 
 bool paged_misaligned(const PagedArgs& a, const void* k_cache, const void* v_cache) {
   return misaligned(k_cache) || misaligned(v_cache) || misaligned4(a.row_start) || misaligned4(a.lens) || misaligned4(a.table) ||
          misaligned4(a.k_scale) || misaligned4(a.v_scale);
+}
+
+// a layer's calls over pages: the cache, and where the attention keeps its partial results
+struct PagedCall {
+  const caat_paged_desc* d;
+  PagedArgs a;
+  void* k;
+  void* v;
+  void* ws;
+};
+
+// One Llama-style decoder layer at inference (which uses the partial channel-reduce too, Sec. 3.2), either for one
+// new token per sequence over a KV cache (decode) or for a whole prompt that fills the cache (prefill, the
+// time-to-first-token workload of Sec. 5.2): RMSNorm -> q,k,v -> RoPE -> store k,v in the cache -> attention
+// (streaming over kv_len+1 keys / causal flash attention over the prompt) -> o_proj -> PCR + residual -> RMSNorm ->
+// SwiGLU MLP -> PCR + residual.  paged: the decode kind's layer over a paged cache, any number of new tokens per sequence.
+int layer_fwd(const caat_desc* d, const caat_ws_layout& L, const void* const* weights, const void* r, void* r_out,
+              void* kv_k, void* kv_v, void* workspace, size_t ws_bytes, void* hip_stream, const PagedCall* paged = nullptr) {
+  const bool prefill = d->kind == CAAT_LAYER_PREFILL;
+  if (!weights || !r || !r_out || !kv_k || !kv_v || !workspace) return CAAT_EINVAL;
+  const void* g_attn = weights[0]; const void* wqkv = weights[1]; const void* wo = weights[2];
+  const void* g_mlp = weights[3]; const void* wgu = weights[4]; const void* wb = weights[5];
+  if (!g_attn || !wqkv || !wo || !g_mlp || !wgu || !wb) return CAAT_EINVAL;
+  if (!(d->rope_base > 0.0f)) return CAAT_EINVAL;
+  if (d->norm != CAAT_RMSNORM || d->head_dim != 128) return CAAT_EUNSUPPORTED;
+  if (paged) {                                                        // the lengths stand on the device
+  } else if (prefill) {
+    if (d->kv_len != 0 || d->kv_cap < d->seq) return CAAT_ESHAPE;     // the prompt starts an empty cache
+  } else {
+    if (d->seq != 1 || d->kv_len < 0 || d->kv_cap <= d->kv_len) return CAAT_ESHAPE;
+  }
+  if (!paged && d->kv_cap * 256 >= 0x7FFFFFFFLL) return CAAT_ESHAPE;
+  if (misaligned(g_attn) || misaligned(wqkv) || misaligned(wo) || misaligned(g_mlp) || misaligned(wgu) || misaligned(wb) ||
+      misaligned(r) || misaligned(r_out) || misaligned(kv_k) || misaligned(kv_v) || misaligned(workspace))
+    return CAAT_EALIGN;
+  if (ws_bytes < (L.bytes_scratch ? L.off_scratch : L.total_bytes)) return CAAT_EWORKSPACE;   // see layer_scratch
+  if (d->tokens == 0) return CAAT_OK;
+  hipStream_t s = (hipStream_t)hip_stream;
+  char* ws = (char*)workspace;
+  const long long T = d->T, n = d->tokens, h = d->h, hpr = d->n_heads / d->T, hd = hpr * d->head_dim, fr = d->ffn / d->T;
+  const long long kvpr = kv_heads_of(d) / d->T, qw = qkv_width(d);
+  bf16_t* X1 = (bf16_t*)(ws + L.off_X1);
+  bf16_t* QKV = (bf16_t*)(ws + L.off_Q);
+  bf16_t* H = (bf16_t*)(ws + L.off_H);
+  bf16_t* R1 = (bf16_t*)(ws + L.off_R1);
+  bf16_t* X2 = (bf16_t*)(ws + L.off_X2);
+  bf16_t* P = (bf16_t*)(ws + L.off_P);
+  bf16_t* Y = (bf16_t*)(ws + L.off_Y);
+  float* rstd = (float*)(ws + L.off_rstd);
+  void* scratch = L.bytes_scratch ? ws + L.off_scratch : nullptr;
+  const size_t scratch_bytes = scratch ? std::min(L.bytes_scratch, ws_bytes - L.off_scratch) : 0;
+  hipError_t e;
+  GemmParams q;
+#define CAAT_STEP(name, call) { ProfScope ps(s, name); e = (call); } if (e != hipSuccess) return CAAT_EHIP;
+  CAAT_STEP("norm_fwd", launch_norm_fwd((const bf16_t*)r, (const bf16_t*)g_attn, nullptr, X1, nullptr, rstd, CAAT_RMSNORM, (int)T,
+                                        n, (int)h, d->eps, s, dedup_hs(d)))
+  std::memset(&q, 0, sizeof(q));
+  q.a = X1; q.lda = h; q.stride_a = n * h;
+  q.b = (const bf16_t*)wqkv; q.ldb = h; q.stride_b = qw * h;
+  q.c = QKV; q.ldc = qw; q.stride_c = n * qw;
+  q.G = (int)T; q.M = (int)n; q.N = (int)qw; q.K = (int)h;
+  q.rope = {(int)d->seq, (int)hpr * 128, (int)kvpr * 128, (int)d->batch, log2f(d->rope_base), (bf16_t*)kv_k, (bf16_t*)kv_v, d->kv_cap};
+  const bool rotate = prefill && rope_in_gemm(q);
+  CAAT_STEP("gemm_nt_qkv", launch_gemm(q, 0, rotate ? EPI_ROPE : EPI_PLAIN, s))
+  if (prefill) {
+    if (!rotate) {
+      CAAT_STEP("rope_kv_append", launch_rope_append(QKV, (bf16_t*)kv_k, (bf16_t*)kv_v, T * d->batch, d->seq, (int)hpr, (int)kvpr,
+                                                     d->head_dim, d->rope_base, d->kv_cap, d->kv_len, s))
+    }
+    CAAT_STEP("flash_attn_fwd", launch_flash_fwd(QKV, H, nullptr, T * d->batch, d->seq, (int)hpr, (int)kvpr, d->head_dim, s))
+  } else if (paged) {
+    PagedArgs a = paged->a;
+    a.ld_q = qw;                                // q is rotated where it lies
+    const int e4m3 = paged->d->cache_type == CAAT_CACHE_E4M3;
+    CAAT_STEP("paged_append", launch_paged_append(a, e4m3, QKV, QKV, qw, paged->k, paged->v, paged->d->rope_base, s))
+    CAAT_STEP("paged_attn", launch_paged_attn(a, e4m3, QKV, H, paged->k, paged->v, paged->d->max_new, paged->ws, s))
+  } else {
+    // decode: the attention kernel rotates q and the new k itself, appends k, v to the caches and attends to
+    // kv_len cached keys plus the new one
+    CAAT_STEP("decode_attn", launch_decode_attn(QKV, (bf16_t*)kv_k, (bf16_t*)kv_v, H, T * n, (int)hpr, (int)kvpr,
+                                                d->head_dim, d->kv_cap, d->kv_len + 1, d->rope_base,
+                                                scratch, scratch_bytes, s))
+  }
+  // the reduce after o_proj and the RMSNorm in front of the MLP run as one launch where the fused kernel takes the
+  // shape: for decode-sized batches both are start-up latency, for prompts the fused kernel does not read the
+  // reduced shared channels back from memory (measured 1.28 ms instead of 0.61 + 0.78 ms on 16 prompts of 2048)
+  const bool fuse_mid = fuse_reduce_norm(d), spread = spread_reduce_norm(d, scratch_bytes);
+  {
+    const int st = rowpar_pcr(d, H, hd, (const bf16_t*)wo, (const bf16_t*)r, spread ? (bf16_t*)scratch : R1, scratch,
+                              scratch_bytes, s, fuse_mid);
+    if (st != CAAT_OK) return st;
+  }
+  if (spread) {
+    CAAT_STEP("partial_sync_norm_fwd", launch_sync_norm_rank((const bf16_t*)scratch, (const bf16_t*)r, (const bf16_t*)g_mlp, R1, X2,
+                                                             rstd, (int)T, n, (int)h, d->hs, d->eps, s))
+  } else if (fuse_mid) {
+    CAAT_STEP("partial_sync_norm_fwd", launch_sync_norm(R1, (const bf16_t*)r, (const bf16_t*)g_mlp, nullptr, X2, nullptr, rstd,
+                                                        CAAT_RMSNORM, (int)T, n, (int)h, d->hs, d->eps, s))
+  } else {
+    CAAT_STEP("norm_fwd", launch_norm_fwd(R1, (const bf16_t*)g_mlp, nullptr, X2, nullptr, rstd, CAAT_RMSNORM, (int)T, n, (int)h,
+                                          d->eps, s, dedup_hs(d)))
+  }
+  std::memset(&q, 0, sizeof(q));
+  q.a = X2; q.lda = h; q.stride_a = n * h;
+  q.b = (const bf16_t*)wgu; q.ldb = h; q.stride_b = 2 * fr * h;
+  q.c = P; q.ldc = 2 * fr; q.stride_c = n * 2 * fr;
+  q.c2 = Y; q.ldc2 = fr; q.stride_c2 = n * fr;
+  q.G = (int)T; q.M = (int)n; q.N = (int)fr; q.K = (int)h; q.half = (int)fr;
+  CAAT_STEP("gemm_nt_swiglu_fwd", launch_gemm(q, 0, EPI_SWIGLU_FWD, s))
+  {
+    const int st = rowpar_pcr(d, Y, fr, (const bf16_t*)wb, R1, (bf16_t*)r_out, scratch, scratch_bytes, s);
+    if (st != CAAT_OK) return st;
+  }
+#undef CAAT_STEP
+  return CAAT_OK;
 }
 
 }  // namespace
@@ -883,6 +899,39 @@ int caat_paged_attn(const caat_paged_desc* d, const void* q, void* out, const in
   ProfScope ps((hipStream_t)hip_stream, "paged_attn");
   return hip_status(launch_paged_attn(a, d->cache_type == CAAT_CACHE_E4M3, (const bf16_t*)q, (bf16_t*)out, k_cache, v_cache,
                                       d->max_new, workspace, (hipStream_t)hip_stream));
+}
+
+size_t caat_paged_layer_workspace_bytes(const caat_desc* d, const caat_paged_desc* pages) {
+  caat_ws_layout L;
+  PagedArgs a;
+  static const int some = 0;
+  if (layout_of(d, &L) != CAAT_OK || d->kind != CAAT_ATTN_DECODE || paged_args(pages, &some, nullptr, nullptr, nullptr, nullptr, &a) != CAAT_OK)
+    return 0;
+  return align256(L.total_bytes) + paged_attn_workspace_bytes(a, pages->max_new);
+}
+
+int caat_paged_layer_fwd(const caat_desc* d, const caat_paged_desc* pages, const void* const* weights, const void* r, void* r_out,
+                         const int* row_start, const int* lens, const int* page_table, void* k_cache, void* v_cache,
+                         const float* k_scale, const float* v_scale, void* workspace, size_t ws_bytes, void* hip_stream) {
+  caat_ws_layout L;
+  int st = layout_of(d, &L);
+  if (st != CAAT_OK) return st;
+  PagedCall call;
+  st = paged_args(pages, row_start, lens, page_table, k_scale, v_scale, &call.a);
+  if (st != CAAT_OK) return st;
+  if (d->kind != CAAT_ATTN_DECODE || !(pages->rope_base > 0.0f) || d->rope_base != pages->rope_base) return CAAT_EINVAL;
+  if (d->T != pages->T || d->n_heads != pages->n_heads || kv_heads_of(d) / d->T != call.a.kvpr || d->head_dim != pages->head_dim ||
+      d->tokens != pages->rows || d->seq != 1 || pages->ld_q != 0 || pages->ld_qkv != 0)
+    return CAAT_ESHAPE;
+  if (!lens || !page_table || !k_cache || !v_cache) return CAAT_EINVAL;
+  if (paged_misaligned(call.a, k_cache, v_cache)) return CAAT_EALIGN;
+  const size_t own = align256(L.total_bytes), attn = paged_attn_workspace_bytes(call.a, pages->max_new);
+  if (workspace && ws_bytes < own + attn) return CAAT_EWORKSPACE;
+  call.d = pages;
+  call.k = k_cache;
+  call.v = v_cache;
+  call.ws = attn > 0 && workspace ? (char*)workspace + own : nullptr;
+  return layer_fwd(d, L, weights, r, r_out, k_cache, v_cache, workspace, own, hip_stream, &call);
 }
 
 int caat_block_bwd(const caat_desc* d, const void* const* weights, const void* x, const void* r_out, void* workspace,

@@ -65,3 +65,30 @@ def test_arguments_that_are_refused():
         B.paged_append(_desc(T=0), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, stream=0)
     with pytest.raises(B.CaatError):
         B.paged_attn(_desc(T=0), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, None, stream=0)
+
+
+def test_layer_arguments_that_are_refused():
+    from paper_2506_19645_amd import inputs as I
+    cfg = I.BlockConfig("dec", I.KIND_DECODE, I.NORM_RMSNORM, h=1024, T=2, p=0.5, batch=10, seq=1, ffn=512, n_heads=8, head_dim=128,
+                        n_kv_heads=4)
+    call = lambda d, pg, ws=Workspace(1 << 40), w=[FAKE] * 6, r=FAKE, lens=FAKE, k=FAKE, ks=None: B.paged_layer_fwd(
+        d, pg, w, r, FAKE, FAKE, lens, FAKE, k, FAKE, ws, ks, None, stream=0, check=False)
+    good = B.make_desc(cfg)
+    size = B.paged_layer_workspace_bytes(good, _desc())
+    assert size >= B.workspace_bytes(good) + B.paged_attn_workspace_bytes(_desc())
+    assert call(good, _desc(), ws=Workspace(size - 1)) == B.EWORKSPACE and call(good, _desc(), ws=None) == B.EINVAL
+    for field, value, status in (("T", 1, B.ESHAPE), ("n_heads", 16, B.ESHAPE), ("n_kv_heads", 8, B.ESHAPE), ("rows", 11, B.ESHAPE),
+                                 ("ld_q", 1024, B.ESHAPE), ("ld_qkv", 2048, B.ESHAPE), ("rope_base", 500.0, B.EINVAL),
+                                 ("page_size", 8, B.ESHAPE), ("cache_type", 3, B.EINVAL)):
+        assert call(good, _desc(**{field: value})) == status
+    prefill = B.make_desc(cfg.with_(kind=I.KIND_PREFILL, batch=2, seq=5))
+    assert call(prefill, _desc()) == B.EINVAL and B.paged_layer_workspace_bytes(prefill, _desc()) == 0
+    assert B.paged_layer_workspace_bytes(good, _desc(T=0)) == 0
+    assert call(good, _desc(), lens=None) == B.EINVAL and call(good, _desc(), r=None) == B.EINVAL
+    assert call(good, _desc(), k=None) == B.EINVAL and call(good, _desc(), k=FAKE + 8) == B.EALIGN
+    assert call(good, _desc(), ks=FAKE) == B.EINVAL and call(good, _desc(), w=[FAKE] * 5 + [None]) == B.EINVAL
+    norm = B.make_desc(cfg)
+    norm.norm = B.LAYERNORM
+    assert call(norm, _desc()) == B.EUNSUPPORTED
+    with pytest.raises(B.CaatError):
+        B.paged_layer_fwd(prefill, _desc(), [FAKE] * 6, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, None, stream=0)
