@@ -121,8 +121,9 @@ hipError_t launch_paged_append(const PagedArgs& a, int e4m3, const bf16_t* qkv, 
                                float rope_base, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
   RopeTable rt;
-  for (int j = 0; j < 64; ++j) {
-    const double rev = exp2(-2.0 * j / PHD * log2((double)rope_base)) / 6.283185307179586476925;
+  const double step = exp2(-2.0 / PHD * log2((double)rope_base));
+  double rev = 1.0 / 6.283185307179586476925;
+  for (int j = 0; j < 64; ++j, rev *= step) {    // 63 roundings to 53 bits
     rt.rev[j].x = (float)rev;
     rt.rev[j].y = (float)(rev - (double)rt.rev[j].x);
   }
