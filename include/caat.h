@@ -301,7 +301,7 @@ typedef struct caat_paged_desc {
   int page_size;        /* positions per page, a multiple of 16 */
   int max_pages;        /* columns of page_table; max_pages * page_size at most 2^30 */
   long long n_pages;    /* pages of a rank's pool */
-  long long rows;       /* token rows per rank of qkv, q and out */
+  long long rows;       /* token rows per rank of qkv, q and out; at most 2^23, and (rows / 128 + batch + 1) * n_heads as well */
   int max_new;          /* the most new tokens a sequence has in these calls: chooses the kernel, results do not depend on it
                            beyond their rounding */
   float rope_base;      /* caat_paged_append: > 0 */

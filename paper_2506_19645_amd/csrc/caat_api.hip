@@ -454,8 +454,8 @@ int paged_args(const caat_paged_desc* d, const int* row_start, const int* lens, 
     if (st[3] < 128 || st[3] >= (MAX + 1) / 32) return CAAT_ESHAPE;
   }
   if ((d->ld_q && (d->ld_q < hd || d->ld_q % 8 != 0)) || (d->ld_qkv && (d->ld_qkv < qw || d->ld_qkv % 8 != 0))) return CAAT_ESHAPE;
-  // grids and row numbers are 32-bit
-  if (d->rows > MAX || d->rows * hpr > MAX || d->T * hpr > 65535 || (d->rows / 128 + d->batch + 1) * d->T * hpr > MAX) return CAAT_ESHAPE;
+  // a launch has at most 2^24 workgroups of 256 threads
+  if (d->rows > (1LL << 23) || d->T * hpr > 65535 || (d->rows / 128 + d->batch + 1) * d->T * hpr > (1LL << 23)) return CAAT_ESHAPE;
   a->row_start = row_start;
   a->lens = lens;
   a->table = page_table;
@@ -872,7 +872,6 @@ int caat_paged_append(const caat_paged_desc* d, const void* qkv, void* q_out, co
   if (misaligned(qkv) || misaligned(q_out) || paged_misaligned(a, k_cache, v_cache)) return CAAT_EALIGN;
   const long long ld_qkv = d->ld_qkv ? d->ld_qkv : (long long)(a.hpr + 2 * a.kvpr) * 128;
   if (q_out == qkv && a.ld_q != ld_qkv) return CAAT_ESHAPE;
-  ProfScope ps((hipStream_t)hip_stream, "paged_append");
   return hip_status(launch_paged_append(a, d->cache_type == CAAT_CACHE_E4M3, (const bf16_t*)qkv, (bf16_t*)q_out, ld_qkv, k_cache,
                                         v_cache, d->rope_base, (hipStream_t)hip_stream));
 }
@@ -896,7 +895,6 @@ int caat_paged_attn(const caat_paged_desc* d, const void* q, void* out, const in
   if (misaligned(q) || misaligned(out) || paged_misaligned(a, k_cache, v_cache) || (need > 0 && misaligned(workspace)))
     return CAAT_EALIGN;
   if (ws_bytes < need) return CAAT_EWORKSPACE;
-  ProfScope ps((hipStream_t)hip_stream, "paged_attn");
   return hip_status(launch_paged_attn(a, d->cache_type == CAAT_CACHE_E4M3, (const bf16_t*)q, (bf16_t*)out, k_cache, v_cache,
                                       d->max_new, workspace, (hipStream_t)hip_stream));
 }

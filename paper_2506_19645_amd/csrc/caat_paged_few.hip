@@ -61,8 +61,10 @@ struct SeqChunk {
 // workgroup; neither leaves anything for the second kernel.
 enum FewMode { FEW_LINE = 0, FEW_WAVE = 1, FEW_WG = 2 };
 // A unit's start (its queries' and pages' way, the first block's, its results) takes a wave about as long as FSTART blocks: they
-// stand in the line in front of the unit's own.  While there are at most FWIDE units, a stretch belongs to a workgroup, whose
-// waves take a quarter of its blocks each and join their results in LDS, so that a quarter as many go through the workspace.
+// stand in the line in front of the unit's own.  Where units have FWIDE blocks and more on average, a stretch belongs to a workgroup,
+// whose waves take a quarter of a unit's blocks each and join their results in LDS, so that a quarter as many go through the
+// workspace (us, a wave's stretches / a workgroup's: 32 heads, 63 x 2048 keys 368 / 322, 128 x 512 170 / 169, 128 x 256 88 / 94;
+// 64 / 8 heads, 48 of up to 16384 145 / 140; 58 of 19, 16 heads 20 / 32).
 static constexpr int FSTART = 3;
 static constexpr int FWIDE = 24;
 
@@ -124,8 +126,9 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
   const int x0 = (int)min((long long)taker * per, (long long)total), x1 = min(total - x0, per) + x0;
   FewJoin join = {};
   if (x0 < x1) {
-    // the sequence of place x0: `base` is where its first unit begins, unit0 the number of that unit.  (There is one, unless the
-    // list of rows gives some twice and the line is longer than 31 bits: then this wave does nothing.)
+    // the sequence of place x0: `base` is where its first unit begins, unit0 the number of that unit.  (A list that gives rows to
+    // many sequences can make the line longer than 31 bits, and what stands here wrong: the checks that follow keep
+    // such a wave inside the buffers.)
     int b = a.batch, unit0 = 0, base = 0;
     while (sq.at < a.batch) {
       const unsigned long long over = __ballot(base + work_to * heads > x0);
@@ -157,6 +160,7 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
       const int unit = base + u * nb;            // place of the unit
       const int to = min(unit + nb, x1);         // and of the stretch's part of it: x .. to - 1
       const int h = (int)((unsigned)u / (unsigned)tiles), tile = u - h * tiles;
+      if (h >= heads) break;                     // (rows given twice, see above)
       const int rank = h / a.kvpr, kvh = h - rank * a.kvpr;
       // its blocks of keys
       int k0 = 0, k1 = nblk;
@@ -457,7 +461,7 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
         }
       };
       const float vs = E4M3 && a.v_scale ? a.v_scale[h] : 1.0f;
-      if (lane == 0 && unit0 + u < unit_joins && begins) {
+      if (lane == 0 && (unsigned)(unit0 + u) < (unsigned)unit_joins && begins) {
         FewJoin* j = joins + unit0 + u;
         if (all_here) j->rows = 0;
         else *j = FewJoin{rows, rank, kvh, first, tile * ROWS, unit + start_blocks, unit + nb, wide ? -per : per};
@@ -482,7 +486,8 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
           }
         }
       } else {
-        if (begins && !all_here) join = FewJoin{rows, rank, kvh, first, tile * ROWS, unit + start_blocks, unit + nb, per};
+        if (begins && !all_here && (!wide || wave == 0))
+          join = FewJoin{rows, rank, kvh, first, tile * ROWS, unit + start_blocks, unit + nb, wide ? -per : per};
         const int wg0 = blockIdx.x * FNW * per;
         if (wide || (unit + start_blocks <= wg0 && wg0 + FNW * per <= unit + nb)) {
           // the workgroup's waves all work at this unit: joined here, one (partial) result
@@ -550,7 +555,7 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
     }
   }
   if (unit_joins) {                              // the launch has room for unit_joins units
-    for (int i = units + wid * 64 + lane; i < unit_joins; i += gridDim.x * FNW * 64) joins[i].rows = 0;
+    for (int i = max(units, 0) + wid * 64 + lane; i < unit_joins; i += gridDim.x * FNW * 64) joins[i].rows = 0;
   } else if (mode == FEW_LINE && lane == 0) {
     joins[wid] = join;
   }

@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
     }
     total *= heads;                              // (the host has checked that this is below 2^31)
     units *= heads;
-    for (int i = units + taker * 256 + tid; i < line_room; i += gridDim.x * 256) joins[i].rows = 0;
+    for (int i = max(units, 0) + taker * 256 + tid; i < line_room; i += gridDim.x * 256) joins[i].rows = 0;
     per = max((int)((unsigned)(total + gridDim.x - 1) / gridDim.x), PLEAST);
     x = (int)min((long long)taker * per, (long long)total);
     x1 = min(total - x, per) + x;
@@ -161,9 +161,11 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
       base += __builtin_amdgcn_readlane(incl, 63) * heads;
       unit0 += __builtin_amdgcn_readlane(uincl, 63) * heads;
     }
-    if (b < 0) return;                           // (a list that gives rows twice and is longer than 31 bits)
+    // (A list that gives rows to many sequences can make the line longer than 31 bits: then there may be none, or a wrong one.)
+    if (b < 0 || x < base) return;
     const int one = sq.before(sq.tiles);
     h = (int)((unsigned)(x - base) / (unsigned)one);
+    if (h >= heads) return;
     const int r = x - base - h * one;
     for (tile = 0; tile + 64 <= sq.tiles && sq.before(tile + 64) <= r; tile += 64) {}
     tile += __popcll(__ballot(tile + lane < sq.tiles && sq.before(tile + lane) <= r)) - 1;
@@ -171,446 +173,448 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
   const float scale0 = scale_log2;
 
   for (bool more = false;; more = true) {        // the tiles of the stretch
-  const int n = sq.n, first = sq.first, len = sq.len;
-  const int rank = h / a.kvpr, kvh = h - rank * a.kvpr;
-  const int keys = min(len, cap);
-  const int row0 = tile * PBQ;
-  const int kv_end = tile_end(n, len, tile);     // may be 0 or less
-  const int all_blk = max(0, (kv_end + PBK - 1) / PBK);
-  // its blocks that are this workgroup's: blk0 .. blk0 + nblk - 1
-  int begin = 0, end = 1, blk0 = 0, blk1 = all_blk;
-  if (LINE) {
-    end = base + h * sq.before(sq.tiles) + sq.before(tile + 1);
-    const int length = sq.length(tile) - PSTART;
-    begin = end - length;
-    if (x1 <= begin) break;                      // the stretch ends in front of the first one
-    blk0 = (int)((long long)all_blk * (max(x, begin) - begin) / length);
-    blk1 = (int)((long long)all_blk * (min(x1, end) - begin) / length);
-  }
-  const bool begins = x <= begin, all_here = begins && x1 >= end;
-  const int nblk = blk1 - blk0;
-  const int key0 = blk0 * PBK;
-  if (LINE && more) __syncthreads();                     // everyone is done with the last tile's blocks
+    const int n = sq.n, first = sq.first, len = sq.len;
+    const int rank = h / a.kvpr, kvh = h - rank * a.kvpr;
+    const int keys = min(len, cap);
+    const int row0 = tile * PBQ;
+    const int kv_end = tile_end(n, len, tile);     // may be 0 or less
+    const int all_blk = max(0, (kv_end + PBK - 1) / PBK);
+    // its blocks that are this workgroup's: blk0 .. blk0 + nblk - 1
+    int begin = 0, end = 1, blk0 = 0, blk1 = all_blk;
+    if (LINE) {
+      end = base + h * sq.before(sq.tiles) + sq.before(tile + 1);
+      const int length = sq.length(tile) - PSTART;
+      begin = end - length;
+      if (x1 <= begin) break;                      // the stretch ends in front of the first one
+      blk0 = (int)((long long)all_blk * (max(x, begin) - begin) / length);
+      blk1 = (int)((long long)all_blk * (min(x1, end) - begin) / length);
+    }
+    const bool begins = x <= begin, all_here = begins && x1 >= end;
+    const int nblk = blk1 - blk0;
+    const int key0 = blk0 * PBK;
+    if (LINE && more) __syncthreads();                     // everyone is done with the last tile's blocks
 
-  // ---- Q fragments: B operand of S^T = K q^T: lane (row frow, k-half hf) holds q[16 ks + 8 hf .. + 7]
-  const int qr = row0 + wave * 32 + frow;
-  const int token = qr / grp, head = kvh * grp + (qr - token * grp);
-  const bool row_ok = token < n;
-  const long long qrow = (long long)rank * a.rows + first + token;
-  const int lim = row_ok ? (int)min((long long)len - n + token + 1, (long long)keys) : kv_end;
-  const int wave_lim = uni((int)min((long long)len - n + (row0 + wave * 32) / grp + 1, (long long)keys));   // of the wave's first row
-  bf16x8_t qf[PHD / 16];
-  const bf16_t* src = q + (row_ok ? qrow * a.ld_q + head * PHD : 0) + hf * 8;   // rows of nobody: any row, not stored
+    // ---- Q fragments: B operand of S^T = K q^T: lane (row frow, k-half hf) holds q[16 ks + 8 hf .. + 7]
+    const int qr = row0 + wave * 32 + frow;
+    const int token = qr / grp, head = kvh * grp + (qr - token * grp);
+    const bool row_ok = token < n;
+    const long long qrow = (long long)rank * a.rows + first + token;
+    const int lim = row_ok ? (int)min((long long)len - n + token + 1, (long long)keys) : kv_end;
+    const int wave_lim = uni((int)min((long long)len - n + (row0 + wave * 32) / grp + 1, (long long)keys));   // of the wave's first row
+    bf16x8_t qf[PHD / 16];
+    const bf16_t* src = q + (row_ok ? qrow * a.ld_q + head * PHD : 0) + hf * 8;   // rows of nobody: any row, not stored
 #pragma unroll
-  for (int ks = 0; ks < PHD / 16; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(src + ks * 16);
-  scale_log2 = E4M3 && a.k_scale ? scale0 * a.k_scale[h] : scale0;
+    for (int ks = 0; ks < PHD / 16; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(src + ks * 16);
+    scale_log2 = E4M3 && a.k_scale ? scale0 * a.k_scale[h] : scale0;
 
-  f32x16_t oacc[PHD / 32];
+    f32x16_t oacc[PHD / 32];
 #pragma unroll
-  for (int t = 0; t < PHD / 32; ++t)
+    for (int t = 0; t < PHD / 32; ++t)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) oacc[t][r] = 0.0f;
-  float m_run = -INFINITY, l_run = 0.0f;         // running maximum (raw score units) and this lane's share of the row sum
+      for (int r = 0; r < 16; ++r) oacc[t][r] = 0.0f;
+    float m_run = -INFINITY, l_run = 0.0f;         // running maximum (raw score units) and this lane's share of the row sum
 
-  // ---- pages.  `next` holds the table's entries of the 4 groups of 16 keys of block (col, in) that is copied next; a block's
-  // places are made from them when its K is copied and kept for its V, one block later.
-  const const_c_t table = (const_c_t)(a.table + (long long)b * a.max_pages);
-  const int gpp = a.page_size >> 4;              // groups per page
-  const int n_pages = (int)a.n_pages;            // (the host has checked that it fits)
-  const unsigned last_col = (unsigned)(a.max_pages - 1) * 4;
-  const long long page_bytes = a.s_page * ELT, group_bytes = 16 * a.s_row * ELT;
-  const bool quad = (gpp & 3) == 0;              // a block lies inside one page
-  int next[4], nin;                              // entries; group inside its page behind them
-  unsigned ncol;                                 // and byte offset of its column
-  int pin;                                       // group inside its page of the block that is placed next (e4m3: the wave's group),
-  long long pat;                                 // and its byte offset there
-  {
-    const int col = blk0 * 4 / gpp;
-    nin = blk0 * 4 - col * gpp;
-    ncol = min((unsigned)col * 4, last_col);
-    pin = E4M3 ? (nin + wave) % gpp : nin;
-    pat = pin * group_bytes;
-  }
-  const int step = 4 % gpp;
-  auto fetch = [&] {
-    if (quad) {
-      next[0] = *(const_i_t)(table + ncol);
-      if ((nin += 4) == gpp) {
-        nin = 0;
-        ncol = min(ncol + 4, last_col);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        next[i] = *(const_i_t)(table + ncol);
-        if (++nin == gpp) {
+    // ---- pages.  `next` holds the table's entries of the 4 groups of 16 keys of block (col, in) that is copied next; a block's
+    // places are made from them when its K is copied and kept for its V, one block later.
+    const const_c_t table = (const_c_t)(a.table + (long long)b * a.max_pages);
+    const int gpp = a.page_size >> 4;              // groups per page
+    const int n_pages = (int)a.n_pages;            // (the host has checked that it fits)
+    const unsigned last_col = (unsigned)(a.max_pages - 1) * 4;
+    const long long page_bytes = a.s_page * ELT, group_bytes = 16 * a.s_row * ELT;
+    const bool quad = (gpp & 3) == 0;              // a block lies inside one page
+    int next[4], nin;                              // entries; group inside its page behind them
+    unsigned ncol;                                 // and byte offset of its column
+    int pin;                                       // group inside its page of the block that is placed next (e4m3: the wave's group),
+    long long pat;                                 // and its byte offset there
+    {
+      const int col = blk0 * 4 / gpp;
+      nin = blk0 * 4 - col * gpp;
+      ncol = min((unsigned)col * 4, last_col);
+      pin = E4M3 ? (nin + wave) % gpp : nin;
+      pat = pin * group_bytes;
+    }
+    const int step = 4 % gpp;
+    auto fetch = [&] {
+      if (quad) {
+        next[0] = *(const_i_t)(table + ncol);
+        if ((nin += 4) == gpp) {
           nin = 0;
           ncol = min(ncol + 4, last_col);
         }
-      }
-    }
-  };
-  struct Place {
-    long long at[E4M3 ? 1 : 4];                  // byte offsets of the groups (e4m3: of the wave's) inside a head's pages
-    unsigned have;                               // groups that have a page
-  };
-  auto place = [&] {
-    Place p;
-    if constexpr (E4M3) {
-      int mine = next[0];
-      if (quad) {
-        p.have = (unsigned)next[0] < (unsigned)n_pages ? 15u : 0u;
       } else {
-        p.have = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p.have |= (unsigned)next[i] < (unsigned)n_pages ? 1u << i : 0u;
-        mine = wave == 0 ? next[0] : wave == 1 ? next[1] : wave == 2 ? next[2] : next[3];
+        for (int i = 0; i < 4; ++i) {
+          next[i] = *(const_i_t)(table + ncol);
+          if (++nin == gpp) {
+            nin = 0;
+            ncol = min(ncol + 4, last_col);
+          }
+        }
       }
-      p.at[0] = (unsigned)mine < (unsigned)n_pages ? (unsigned)mine * page_bytes + pin * group_bytes : 0;
-      pin += quad ? 4 : step;
-      if (pin >= gpp) pin -= gpp;
-    } else if (quad) {
-      const bool ok = (unsigned)next[0] < (unsigned)n_pages;
-      p.have = ok ? 15u : 0u;
-      p.at[0] = ok ? (unsigned)next[0] * page_bytes + pat : 0;
+    };
+    struct Place {
+      long long at[E4M3 ? 1 : 4];                  // byte offsets of the groups (e4m3: of the wave's) inside a head's pages
+      unsigned have;                               // groups that have a page
+    };
+    auto place = [&] {
+      Place p;
+      if constexpr (E4M3) {
+        int mine = next[0];
+        if (quad) {
+          p.have = (unsigned)next[0] < (unsigned)n_pages ? 15u : 0u;
+        } else {
+          p.have = 0;
 #pragma unroll
-      for (int i = 1; i < 4; ++i) p.at[i] = p.at[i - 1] + group_bytes;
-      pat += 4 * group_bytes;
-      if ((pin += 4) == gpp) {
-        pin = 0;
-        pat = 0;
-      }
-    } else {
-      p.have = 0;
+          for (int i = 0; i < 4; ++i) p.have |= (unsigned)next[i] < (unsigned)n_pages ? 1u << i : 0u;
+          mine = wave == 0 ? next[0] : wave == 1 ? next[1] : wave == 2 ? next[2] : next[3];
+        }
+        p.at[0] = (unsigned)mine < (unsigned)n_pages ? (unsigned)mine * page_bytes + pin * group_bytes : 0;
+        pin += quad ? 4 : step;
+        if (pin >= gpp) pin -= gpp;
+      } else if (quad) {
+        const bool ok = (unsigned)next[0] < (unsigned)n_pages;
+        p.have = ok ? 15u : 0u;
+        p.at[0] = ok ? (unsigned)next[0] * page_bytes + pat : 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool ok = (unsigned)next[i] < (unsigned)n_pages;
-        p.at[i] = ok ? (unsigned)next[i] * page_bytes + pat : 0;
-        p.have |= ok ? 1u << i : 0u;
-        pat += group_bytes;
-        if (++pin == gpp) {
+        for (int i = 1; i < 4; ++i) p.at[i] = p.at[i - 1] + group_bytes;
+        pat += 4 * group_bytes;
+        if ((pin += 4) == gpp) {
           pin = 0;
           pat = 0;
         }
+      } else {
+        p.have = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool ok = (unsigned)next[i] < (unsigned)n_pages;
+          p.at[i] = ok ? (unsigned)next[i] * page_bytes + pat : 0;
+          p.have |= ok ? 1u << i : 0u;
+          pat += group_bytes;
+          if (++pin == gpp) {
+            pin = 0;
+            pat = 0;
+          }
+        }
       }
-    }
-    return p;
-  };
-  const unsigned char* kh = (const unsigned char*)kc + (rank * a.s_rank + kvh * a.s_head) * ELT;
-  const unsigned char* vh = (const unsigned char*)vc + (rank * a.s_rank + kvh * a.s_head) * ELT;
+      return p;
+    };
+    const unsigned char* kh = (const unsigned char*)kc + (rank * a.s_rank + kvh * a.s_head) * ELT;
+    const unsigned char* vh = (const unsigned char*)vc + (rank * a.s_rank + kvh * a.s_head) * ELT;
 
-  // ---- global -> LDS.  bf16: a copy fills 4 rows, the wave's rows 4 wave .. + 3 of each of the 4 groups.  e4m3: a copy fills 8 rows,
-  // a wave takes the group of its number, K and V.
-  const unsigned row_bytes = (unsigned)(a.s_row * ELT);
-  unsigned dko, dvo, dro = 0;
-  {
-    const int row = wave * 4 + (lane >> 4), phys = lane & 15;
-    dko = row * row_bytes + pk_swz(row, phys) * 16;       // (the swizzles repeat every 16 rows)
-    dvo = row * row_bytes + pv_swz(row, phys) * 16;
-    if (E4M3) dro = (lane >> 3) * row_bytes + (lane & 7) * 16;
-  }
-  auto issue_rows = [&](const unsigned char* base, unsigned off, const Place& p, int blk, uint4* t) {
-    uint4* to = t + wave * 4 * PCH;
-    const int left = kv_end - key0 - blk * PBK;  // rows from here on that anybody sees
-    if (left >= PBK && p.have == 15u) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) dma16(make_rsrc(base + p.at[i]), off, to + i * 16 * PCH);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        dma16(make_rsrc(base + p.at[i]), (p.have >> i & 1) && i * 16 + wave * 4 + (lane >> 4) < left ? off : 0x80000000u, to + i * 16 * PCH);
+    // ---- global -> LDS.  bf16: a copy fills 4 rows, the wave's rows 4 wave .. + 3 of each of the 4 groups.  e4m3: a copy fills 8 rows,
+    // a wave takes the group of its number, K and V.
+    const unsigned row_bytes = (unsigned)(a.s_row * ELT);
+    unsigned dko, dvo, dro = 0;
+    {
+      const int row = wave * 4 + (lane >> 4), phys = lane & 15;
+      dko = row * row_bytes + pk_swz(row, phys) * 16;       // (the swizzles repeat every 16 rows)
+      dvo = row * row_bytes + pv_swz(row, phys) * 16;
+      if (E4M3) dro = (lane >> 3) * row_bytes + (lane & 7) * 16;
     }
-  };
-  uint4* raw = smem + 4 * PTILE + (E4M3 ? wave * 256 : 0);
-  auto issue_raw = [&](const unsigned char* base, const Place& p, int blk, uint4* t) {   // the wave's group
-    const int left = p.have >> wave & 1 ? kv_end - key0 - blk * PBK - wave * 16 : 0;
-    const i32x4_t rs = make_rsrc(base + p.at[0]);
+    auto issue_rows = [&](const unsigned char* base, unsigned off, const Place& p, int blk, uint4* t) {
+      uint4* to = t + wave * 4 * PCH;
+      const int left = kv_end - key0 - blk * PBK;  // rows from here on that anybody sees
+      if (left >= PBK && p.have == 15u) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      dma16(rs, i * 8 + (lane >> 3) < left ? dro + i * 8 * row_bytes : 0x80000000u, t + i * 64);
-  };
-  // the wave's group of a raw block as bf16 rows of the tile: lane = row (lane / 4) and a quarter of it
-  auto widen = [&](const uint4* src, uint4* tile_at, bool is_v) {
-    const int r = lane >> 2, part = lane & 3, row = wave * 16 + r;
+        for (int i = 0; i < 4; ++i) dma16(make_rsrc(base + p.at[i]), off, to + i * 16 * PCH);
+      } else {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const uint4 w = src[r * 8 + part * 2 + c];
-      const unsigned x[4] = {w.x, w.y, w.z, w.w};
-      unsigned y[8];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        y[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x[i], 1.0f, false));
-        y[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x[i], 1.0f, true));
+        for (int i = 0; i < 4; ++i)
+          dma16(make_rsrc(base + p.at[i]), (p.have >> i & 1) && i * 16 + wave * 4 + (lane >> 4) < left ? off : 0x80000000u, to + i * 16 * PCH);
       }
+    };
+    uint4* raw = smem + 4 * PTILE + (E4M3 ? wave * 256 : 0);
+    auto issue_raw = [&](const unsigned char* base, const Place& p, int blk, uint4* t) {   // the wave's group
+      const int left = p.have >> wave & 1 ? kv_end - key0 - blk * PBK - wave * 16 : 0;
+      const i32x4_t rs = make_rsrc(base + p.at[0]);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int ch = part * 4 + c * 2 + i;
-        tile_at[row * PCH + (is_v ? pv_swz(row, ch) : pk_swz(row, ch))] = make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+      for (int i = 0; i < 2; ++i)
+        dma16(rs, i * 8 + (lane >> 3) < left ? dro + i * 8 * row_bytes : 0x80000000u, t + i * 64);
+    };
+    // the wave's group of a raw block as bf16 rows of the tile: lane = row (lane / 4) and a quarter of it
+    auto widen = [&](const uint4* src, uint4* tile_at, bool is_v) {
+      const int r = lane >> 2, part = lane & 3, row = wave * 16 + r;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const uint4 w = src[r * 8 + part * 2 + c];
+        const unsigned x[4] = {w.x, w.y, w.z, w.w};
+        unsigned y[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          y[2 * i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x[i], 1.0f, false));
+          y[2 * i + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x[i], 1.0f, true));
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int ch = part * 4 + c * 2 + i;
+          tile_at[row * PCH + (is_v ? pv_swz(row, ch) : pk_swz(row, ch))] = make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+        }
       }
-    }
-  };
-  auto kslot = [&](int blk) { return smem + (blk & 1) * PTILE; };
-  auto vslot = [&](int blk) { return smem + (2 + (blk & 1)) * PTILE; };
+    };
+    auto kslot = [&](int blk) { return smem + (blk & 1) * PTILE; };
+    auto vslot = [&](int blk) { return smem + (2 + (blk & 1)) * PTILE; };
 
-  // Per-lane LDS addresses of the fragment reads; slot, key tile and 16-key slice go into the instructions' immediate offsets.
-  //   K fragment (32 rows x one chunk): row = 32 j + frow, logical chunk 2 ks + hf
-  //   V transpose read: row = 16 u + 4 hf + (i16 >> 2) (+ 8), column 32 dt + 16 half + 4 (i16 & 3)
-  constexpr int TILE_BYTES = PTILE * 16;
-  lds_u4_t koff[PHD / 16];
-  lds_c_t voff[PHD / 32];
-  {
-    const lds_c_t lds0 = (lds_c_t)smem;
+    // Per-lane LDS addresses of the fragment reads; slot, key tile and 16-key slice go into the instructions' immediate offsets.
+    //   K fragment (32 rows x one chunk): row = 32 j + frow, logical chunk 2 ks + hf
+    //   V transpose read: row = 16 u + 4 hf + (i16 >> 2) (+ 8), column 32 dt + 16 half + 4 (i16 & 3)
+    constexpr int TILE_BYTES = PTILE * 16;
+    lds_u4_t koff[PHD / 16];
+    lds_c_t voff[PHD / 32];
+    {
+      const lds_c_t lds0 = (lds_c_t)smem;
 #pragma unroll
-    for (int ks = 0; ks < PHD / 16; ++ks) koff[ks] = (lds_u4_t)(lds0 + (frow * PCH + pk_swz(frow, ks * 2 + hf)) * 16);
-    const int i16 = lane & 15, half = (lane >> 4) & 1;
-    const int vrow = 4 * hf + (i16 >> 2);
+      for (int ks = 0; ks < PHD / 16; ++ks) koff[ks] = (lds_u4_t)(lds0 + (frow * PCH + pk_swz(frow, ks * 2 + hf)) * 16);
+      const int i16 = lane & 15, half = (lane >> 4) & 1;
+      const int vrow = 4 * hf + (i16 >> 2);
 #pragma unroll
-    for (int dt = 0; dt < PHD / 32; ++dt) {
-      const int col = dt * 32 + half * 16 + (i16 & 3) * 4;
-      voff[dt] = lds0 + ((vrow * PCH + pv_swz(vrow, col >> 3)) * 16 + (col & 7) * 2);
-    }
-  }
-  const f32x16_t zero16 = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-  const bf16x2_t ones2 = {(__bf16)1.0f, (__bf16)1.0f};
-
-  Place pk, pv;                                  // of the block whose K was copied last, of the one whose V is next
-  unsigned have = 0, have_next = 0;              // groups with a page of the block in the softmax, of the one behind it
-
-  // One key block: the scores of block blk are in `scur`; those of blk + 1 are made into `snext` under its softmax
-  auto key_block = [&](int blk, f32x16_t* scur, f32x16_t* snext, auto slot_c, auto last_c) {
-    constexpr int SLOT = decltype(slot_c)::value;
-    constexpr bool LAST = decltype(last_c)::value;
-    wait_vmcnt<0>();
-    __syncthreads();                             // K(blk + 1) and V(blk) are there; everyone is done with K(blk) and V(blk - 1)
-    if constexpr (E4M3) {
-      // K(blk + 2) and V(blk + 1) lie in the wave's buffer, K(blk + 3) and V(blk + 2) take their place
-      if (blk + 2 < nblk) widen(raw, kslot(blk), false);
-      if (blk + 1 < nblk) widen(raw + 128, vslot(blk + 1), true);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      pv = pk;
-      if (blk + 3 < nblk) {
-        pk = place();
-        fetch();
-        issue_raw(kh, pk, blk + 3, raw);
+      for (int dt = 0; dt < PHD / 32; ++dt) {
+        const int col = dt * 32 + half * 16 + (i16 & 3) * 4;
+        voff[dt] = lds0 + ((vrow * PCH + pv_swz(vrow, col >> 3)) * 16 + (col & 7) * 2);
       }
-      if (blk + 2 < nblk) issue_raw(vh, pv, blk + 2, raw + 128);
-    } else {
-      pv = pk;
-      if (blk + 2 < nblk) {
-        pk = place();
-        fetch();
-        issue_rows(kh, dko, pk, blk + 2, kslot(blk));
-      }
-      if (blk + 1 < nblk) issue_rows(vh, dvo, pv, blk + 1, vslot(blk + 1));
     }
-    const int kv0 = key0 + blk * PBK;
-    // ---- mask (keys of register r: kv0 + 32 j + 8 (r / 4) + 4 hf + r % 4): only where some row of the wave does not see the whole
-    // block, or a group has no page
-    if (kv0 + PBK > wave_lim || have != 15u) {
+    const f32x16_t zero16 = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    const bf16x2_t ones2 = {(__bf16)1.0f, (__bf16)1.0f};
+
+    Place pk, pv;                                  // of the block whose K was copied last, of the one whose V is next
+    unsigned have = 0, have_next = 0;              // groups with a page of the block in the softmax, of the one behind it
+
+    // One key block: the scores of block blk are in `scur`; those of blk + 1 are made into `snext` under its softmax
+    auto key_block = [&](int blk, f32x16_t* scur, f32x16_t* snext, auto slot_c, auto last_c) {
+      constexpr int SLOT = decltype(slot_c)::value;
+      constexpr bool LAST = decltype(last_c)::value;
+      wait_vmcnt<0>();
+      __syncthreads();                             // K(blk + 1) and V(blk) are there; everyone is done with K(blk) and V(blk - 1)
+      if constexpr (E4M3) {
+        // K(blk + 2) and V(blk + 1) lie in the wave's buffer, K(blk + 3) and V(blk + 2) take their place
+        if (blk + 2 < nblk) widen(raw, kslot(blk), false);
+        if (blk + 1 < nblk) widen(raw + 128, vslot(blk + 1), true);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        pv = pk;
+        if (blk + 3 < nblk) {
+          pk = place();
+          fetch();
+          issue_raw(kh, pk, blk + 3, raw);
+        }
+        if (blk + 2 < nblk) issue_raw(vh, pv, blk + 2, raw + 128);
+      } else {
+        pv = pk;
+        if (blk + 2 < nblk) {
+          pk = place();
+          fetch();
+          issue_rows(kh, dko, pk, blk + 2, kslot(blk));
+        }
+        if (blk + 1 < nblk) issue_rows(vh, dvo, pv, blk + 1, vslot(blk + 1));
+      }
+      const int kv0 = key0 + blk * PBK;
+      // ---- mask (keys of register r: kv0 + 32 j + 8 (r / 4) + 4 hf + r % 4): only where some row of the wave does not see the whole
+      // block, or a group has no page
+      if (kv0 + PBK > wave_lim || have != 15u) {
+#pragma unroll
+        for (int j = 0; j < PBK / 32; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int key = kv0 + j * 32 + 8 * (r >> 2) + 4 * hf + (r & 3);
+            if (key >= lim || !(have >> (j * 2 + (r >> 3)) & 1)) scur[j][r] = -INFINITY;
+          }
+      }
+      have = have_next;
+      have_next = E4M3 ? pv.have : pk.have;
+      // ---- one MFMA per step, a scheduling fence behind each:
+      //   steps 0-15 : score MFMAs of block blk + 1 (fragments read three steps ahead); underneath: the row maximum (steps 0-3),
+      //                its exchange with the other half-row (4-5), the exponentials of keys 0-31 (6-13)
+      //   steps 16-31: second-product MFMAs; underneath: the exponentials of keys 32-63 (steps 16-23)
+      auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+      auto kread = [&](int idx) -> u32x4_t { return koff[idx & 7][((SLOT ^ 1) * TILE_BYTES + (idx >> 3) * 32 * PCH * 16) / 16]; };
+      __builtin_amdgcn_s_setprio(1);               // in front of a wave that waits for its copies (e4m3 chunk 332 -> 320 us, others even)
+      float mx = -INFINITY, mxo = 0.0f, m_new = 0.0f, alpha = 1.0f, mb = 0.0f, psum = 0.0f;
+      unsigned pw[PBK / 2];                        // the block's probabilities, bf16 pairs
+      auto prob_pair = [&](int i) {
+        const int j = i >> 3, r = (i & 7) * 2;
+        const float p0 = __builtin_amdgcn_exp2f(scur[j][r] * scale_log2 - mb);
+        const float p1 = __builtin_amdgcn_exp2f(scur[j][r + 1] * scale_log2 - mb);
+        pw[i] = pack2bf(p0, p1);
+        // the row sum takes the probabilities as the second product sees them, two per instruction
+        psum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pw[i]), ones2, psum, false);
+        asm volatile("" : "+v"(pw[i]), "+v"(psum));   // pins the pair to this place in the stream
+      };
+      u32x4_t kr[3];
+      if constexpr (!LAST) {
+        kr[0] = kread(0);
+        kr[1] = kread(1);
+        kr[2] = kread(2);
+      }
+      fence();
+#pragma unroll
+      for (int idx = 0; idx < 16; ++idx) {
+        if constexpr (!LAST) {
+          const int j = idx >> 3, ks = idx & 7;
+          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, kr[idx % 3]);
+          snext[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], ks == 0 ? zero16 : snext[j], 0, 0, 0);
+          if (idx + 3 < 16) kr[idx % 3] = kread(idx + 3);
+        }
+        if (idx < 4) {
+          const int j = idx >> 1, r0 = (idx & 1) * 8;
+#pragma unroll
+          for (int r = 0; r < 8; r += 2) mx = pmax3(mx, scur[j][r0 + r], scur[j][r0 + r + 1]);
+          if (idx == 3) mxo = __shfl_xor(mx, 32, 64);
+        } else if (idx == 5) {
+          m_new = fmaxf(m_run, fmaxf(mx, mxo));
+          const float mz = m_new == -INFINITY ? 0.0f : m_new;   // no key seen so far: nothing is added
+          alpha = __builtin_amdgcn_exp2f((m_run - mz) * scale_log2);
+          mb = mz * scale_log2;
+        } else if (idx >= 6 && idx < 14) {
+          prob_pair(idx - 6);
+        }
+        fence();
+      }
+      if (__any(m_new != m_run)) {                 // the running maximum settles after the first blocks
+#pragma unroll
+        for (int t = 0; t < PHD / 32; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) oacc[t][r] *= alpha;
+      }
+      m_run = m_new;
+
+      // ---- O^T += V^T P^T: k-slice u (16 keys): lane half hf contributes keys 16 u + 4 hf + {0 .. 3} and 16 u + 8 + 4 hf + {0 .. 3}
+      auto vread = [&](int st, short4_t& v0, short4_t& v1) {
+        const lds_c_t a0 = voff[st & 3] + ((2 + SLOT) * TILE_BYTES + (st >> 2) * 16 * PCH * 16);
+        v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t)a0);
+        v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t)(a0 + 8 * PCH * 16));
+      };
+      short4_t va[3], vb[3];
+      vread(0, va[0], vb[0]);
+      vread(1, va[1], vb[1]);
+      vread(2, va[2], vb[2]);
+      fence();
+#pragma unroll
+      for (int st = 0; st < 16; ++st) {
+        const int u = st >> 2, dt = st & 3;
+        const short8_t vv = {va[st % 3][0], va[st % 3][1], va[st % 3][2], va[st % 3][3],
+                             vb[st % 3][0], vb[st % 3][1], vb[st % 3][2], vb[st % 3][3]};
+        const bf16x8_t pfu = __builtin_bit_cast(bf16x8_t, make_uint4(pw[4 * u], pw[4 * u + 1], pw[4 * u + 2], pw[4 * u + 3]));
+        oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vv), pfu, oacc[dt], 0, 0, 0);
+        if (st + 3 < 16) vread(st + 3, va[st % 3], vb[st % 3]);
+        if (st < 8) prob_pair(8 + st);
+        fence();
+      }
+      l_run = l_run * alpha + psum;
+      __builtin_amdgcn_s_setprio(0);
+    };
+
+    if (nblk > 0) {
+      // prologue: K(0) alone first (its scores open the pipeline), then what the first loop iteration expects
+      f32x16_t sa[PBK / 32], sb[PBK / 32];
+      fetch();
+      pk = place();
+      fetch();
+      if constexpr (E4M3) {
+        issue_raw(kh, pk, 0, raw);
+        issue_raw(vh, pk, 0, raw + 128);
+        const unsigned have0 = pk.have;
+        wait_vmcnt<0>();
+        widen(raw, kslot(0), false);
+        widen(raw + 128, vslot(0), true);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        have = have0;
+        if (1 < nblk) {
+          pk = place();
+          fetch();
+          issue_raw(kh, pk, 1, raw);
+          issue_raw(vh, pk, 1, raw + 128);
+          wait_vmcnt<0>();
+          widen(raw, kslot(1), false);             // V(1) stays in the buffer for the first iteration
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          have_next = pk.have;
+          if (2 < nblk) {
+            pk = place();
+            fetch();
+            issue_raw(kh, pk, 2, raw);
+          }
+        }
+        __syncthreads();
+      } else {
+        issue_rows(kh, dko, pk, 0, kslot(0));
+        wait_vmcnt<0>();
+        __syncthreads();
+        have = pk.have;
+        issue_rows(vh, dvo, pk, 0, vslot(0));
+        if (1 < nblk) {
+          pk = place();
+          fetch();
+          issue_rows(kh, dko, pk, 1, kslot(1));
+        }
+        have_next = pk.have;
+      }
+#pragma unroll
+      for (int ks = 0; ks < PHD / 16; ++ks) asm volatile("" : "+v"(qf[ks]));   // the compiler's wait for q stands in front of the loop
 #pragma unroll
       for (int j = 0; j < PBK / 32; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = kv0 + j * 32 + 8 * (r >> 2) + 4 * hf + (r & 3);
-          if (key >= lim || !(have >> (j * 2 + (r >> 3)) & 1)) scur[j][r] = -INFINITY;
+        for (int ks = 0; ks < PHD / 16; ++ks) {
+          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, koff[ks][(j * 32 * PCH * 16) / 16]);
+          sa[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], ks == 0 ? zero16 : sa[j], 0, 0, 0);
         }
-    }
-    have = have_next;
-    have_next = E4M3 ? pv.have : pk.have;
-    // ---- one MFMA per step, a scheduling fence behind each:
-    //   steps 0-15 : score MFMAs of block blk + 1 (fragments read three steps ahead); underneath: the row maximum (steps 0-3),
-    //                its exchange with the other half-row (4-5), the exponentials of keys 0-31 (6-13)
-    //   steps 16-31: second-product MFMAs; underneath: the exponentials of keys 32-63 (steps 16-23)
-    auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
-    auto kread = [&](int idx) -> u32x4_t { return koff[idx & 7][((SLOT ^ 1) * TILE_BYTES + (idx >> 3) * 32 * PCH * 16) / 16]; };
-    float mx = -INFINITY, mxo = 0.0f, m_new = 0.0f, alpha = 1.0f, mb = 0.0f, psum = 0.0f;
-    unsigned pw[PBK / 2];                        // the block's probabilities, bf16 pairs
-    auto prob_pair = [&](int i) {
-      const int j = i >> 3, r = (i & 7) * 2;
-      const float p0 = __builtin_amdgcn_exp2f(scur[j][r] * scale_log2 - mb);
-      const float p1 = __builtin_amdgcn_exp2f(scur[j][r + 1] * scale_log2 - mb);
-      pw[i] = pack2bf(p0, p1);
-      // the row sum takes the probabilities as the second product sees them, two per instruction
-      psum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pw[i]), ones2, psum, false);
-      asm volatile("" : "+v"(pw[i]), "+v"(psum));   // pins the pair to this place in the stream
-    };
-    u32x4_t kr[3];
-    if constexpr (!LAST) {
-      kr[0] = kread(0);
-      kr[1] = kread(1);
-      kr[2] = kread(2);
-    }
-    fence();
-#pragma unroll
-    for (int idx = 0; idx < 16; ++idx) {
-      if constexpr (!LAST) {
-        const int j = idx >> 3, ks = idx & 7;
-        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, kr[idx % 3]);
-        snext[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], ks == 0 ? zero16 : snext[j], 0, 0, 0);
-        if (idx + 3 < 16) kr[idx % 3] = kread(idx + 3);
+      int blk = 0;
+      for (; blk + 2 < nblk; blk += 2) {
+        key_block(blk, sa, sb, std::integral_constant<int, 0>{}, std::false_type{});
+        key_block(blk + 1, sb, sa, std::integral_constant<int, 1>{}, std::false_type{});
       }
-      if (idx < 4) {
-        const int j = idx >> 1, r0 = (idx & 1) * 8;
-#pragma unroll
-        for (int r = 0; r < 8; r += 2) mx = pmax3(mx, scur[j][r0 + r], scur[j][r0 + r + 1]);
-        if (idx == 3) mxo = __shfl_xor(mx, 32, 64);
-      } else if (idx == 5) {
-        m_new = fmaxf(m_run, fmaxf(mx, mxo));
-        const float mz = m_new == -INFINITY ? 0.0f : m_new;   // no key seen so far: nothing is added
-        alpha = __builtin_amdgcn_exp2f((m_run - mz) * scale_log2);
-        mb = mz * scale_log2;
-      } else if (idx >= 6 && idx < 14) {
-        prob_pair(idx - 6);
+      if (blk + 1 < nblk) {
+        key_block(blk, sa, sb, std::integral_constant<int, 0>{}, std::false_type{});
+        key_block(blk + 1, sb, sa, std::integral_constant<int, 1>{}, std::true_type{});
+      } else {
+        key_block(blk, sa, sb, std::integral_constant<int, 0>{}, std::true_type{});
       }
-      fence();
     }
-    if (__any(m_new != m_run)) {                 // the running maximum settles after the first blocks
-#pragma unroll
-      for (int t = 0; t < PHD / 32; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[t][r] *= alpha;
-    }
-    m_run = m_new;
 
-    // ---- O^T += V^T P^T: k-slice u (16 keys): lane half hf contributes keys 16 u + 4 hf + {0 .. 3} and 16 u + 8 + 4 hf + {0 .. 3}
-    auto vread = [&](int st, short4_t& v0, short4_t& v1) {
-      const lds_c_t a0 = voff[st & 3] + ((2 + SLOT) * TILE_BYTES + (st >> 2) * 16 * PCH * 16);
-      v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t)a0);
-      v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t)(a0 + 8 * PCH * 16));
-    };
-    short4_t va[3], vb[3];
-    vread(0, va[0], vb[0]);
-    vread(1, va[1], vb[1]);
-    vread(2, va[2], vb[2]);
-    fence();
-#pragma unroll
-    for (int st = 0; st < 16; ++st) {
-      const int u = st >> 2, dt = st & 3;
-      const short8_t vv = {va[st % 3][0], va[st % 3][1], va[st % 3][2], va[st % 3][3],
-                           vb[st % 3][0], vb[st % 3][1], vb[st % 3][2], vb[st % 3][3]};
-      const bf16x8_t pfu = __builtin_bit_cast(bf16x8_t, make_uint4(pw[4 * u], pw[4 * u + 1], pw[4 * u + 2], pw[4 * u + 3]));
-      oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vv), pfu, oacc[dt], 0, 0, 0);
-      if (st + 3 < 16) vread(st + 3, va[st % 3], vb[st % 3]);
-      if (st < 8) prob_pair(8 + st);
-      fence();
+    // ---- normalise and store: lane holds out[row][32 dt + 8 (r / 4) + 4 hf + r % 4]
+    l_run += __shfl_xor(l_run, 32, 64);
+    if (LINE && begins && tid == 0) {
+      PromptJoin* j = joins + unit0 + h * sq.tiles + tile;
+      if ((unsigned)(unit0 + h * sq.tiles + tile) < (unsigned)line_room)
+        *j = PromptJoin{all_here ? 0 : min(PBQ, n * grp - row0), rank, kvh, first, row0, begin, end, per};
     }
-    l_run = l_run * alpha + psum;
-  };
-
-  if (nblk > 0) {
-    // prologue: K(0) alone first (its scores open the pipeline), then what the first loop iteration expects
-    f32x16_t sa[PBK / 32], sb[PBK / 32];
-    fetch();
-    pk = place();
-    fetch();
-    if constexpr (E4M3) {
-      issue_raw(kh, pk, 0, raw);
-      issue_raw(vh, pk, 0, raw + 128);
-      const unsigned have0 = pk.have;
-      wait_vmcnt<0>();
-      widen(raw, kslot(0), false);
-      widen(raw + 128, vslot(0), true);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      have = have0;
-      if (1 < nblk) {
-        pk = place();
-        fetch();
-        issue_raw(kh, pk, 1, raw);
-        issue_raw(vh, pk, 1, raw + 128);
-        wait_vmcnt<0>();
-        widen(raw, kslot(1), false);             // V(1) stays in the buffer for the first iteration
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        have_next = pk.have;
-        if (2 < nblk) {
-          pk = place();
-          fetch();
-          issue_raw(kh, pk, 2, raw);
-        }
+    if (LINE && !all_here) {
+      const int taker = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+      if (row_ok) {
+        float* o = part + ((2LL * taker + (begins ? 1 : 0)) * PBQ + wave * 32 + frow) * PPR;
+#pragma unroll
+        for (int dt = 0; dt < PHD / 32; ++dt)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<float4*>(o + dt * 32 + k * 8 + hf * 4) =
+                make_float4(oacc[dt][k * 4], oacc[dt][k * 4 + 1], oacc[dt][k * 4 + 2], oacc[dt][k * 4 + 3]);
+        if (hf == 0) *reinterpret_cast<float2*>(o + PHD) = make_float2(m_run * scale_log2, l_run);
       }
-      __syncthreads();
-    } else {
-      issue_rows(kh, dko, pk, 0, kslot(0));
-      wait_vmcnt<0>();
-      __syncthreads();
-      have = pk.have;
-      issue_rows(vh, dvo, pk, 0, vslot(0));
-      if (1 < nblk) {
-        pk = place();
-        fetch();
-        issue_rows(kh, dko, pk, 1, kslot(1));
-      }
-      have_next = pk.have;
-    }
-#pragma unroll
-    for (int ks = 0; ks < PHD / 16; ++ks) asm volatile("" : "+v"(qf[ks]));   // the compiler's wait for q stands in front of the loop
-#pragma unroll
-    for (int j = 0; j < PBK / 32; ++j)
-#pragma unroll
-      for (int ks = 0; ks < PHD / 16; ++ks) {
-        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, koff[ks][(j * 32 * PCH * 16) / 16]);
-        sa[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], ks == 0 ? zero16 : sa[j], 0, 0, 0);
-      }
-    int blk = 0;
-    for (; blk + 2 < nblk; blk += 2) {
-      key_block(blk, sa, sb, std::integral_constant<int, 0>{}, std::false_type{});
-      key_block(blk + 1, sb, sa, std::integral_constant<int, 1>{}, std::false_type{});
-    }
-    if (blk + 1 < nblk) {
-      key_block(blk, sa, sb, std::integral_constant<int, 0>{}, std::false_type{});
-      key_block(blk + 1, sb, sa, std::integral_constant<int, 1>{}, std::true_type{});
-    } else {
-      key_block(blk, sa, sb, std::integral_constant<int, 0>{}, std::true_type{});
-    }
-  }
-
-  // ---- normalise and store: lane holds out[row][32 dt + 8 (r / 4) + 4 hf + r % 4]
-  l_run += __shfl_xor(l_run, 32, 64);
-  if (LINE && begins && tid == 0) {
-    PromptJoin* j = joins + unit0 + h * sq.tiles + tile;
-    if (unit0 + h * sq.tiles + tile < line_room)
-      *j = PromptJoin{all_here ? 0 : min(PBQ, n * grp - row0), rank, kvh, first, row0, begin, end, per};
-  }
-  if (LINE && !all_here) {
-    const int taker = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
-    if (row_ok) {
-      float* o = part + ((2LL * taker + (begins ? 1 : 0)) * PBQ + wave * 32 + frow) * PPR;
+    } else if (row_ok) {
+      const float inv = l_run == 0.0f ? 0.0f : (E4M3 && a.v_scale ? a.v_scale[h] : 1.0f) / l_run;
+      bf16_t* o = out + (qrow * a.hpr + head) * PHD;
 #pragma unroll
       for (int dt = 0; dt < PHD / 32; ++dt)
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          *reinterpret_cast<float4*>(o + dt * 32 + k * 8 + hf * 4) =
-              make_float4(oacc[dt][k * 4], oacc[dt][k * 4 + 1], oacc[dt][k * 4 + 2], oacc[dt][k * 4 + 3]);
-      if (hf == 0) *reinterpret_cast<float2*>(o + PHD) = make_float2(m_run * scale_log2, l_run);
+        for (int k = 0; k < 4; ++k) {
+          uint2 w;
+          w.x = pack2bf(oacc[dt][k * 4 + 0] * inv, oacc[dt][k * 4 + 1] * inv);
+          w.y = pack2bf(oacc[dt][k * 4 + 2] * inv, oacc[dt][k * 4 + 3] * inv);
+          *reinterpret_cast<uint2*>(o + dt * 32 + k * 8 + hf * 4) = w;
+        }
     }
-  } else if (row_ok) {
-    const float inv = l_run == 0.0f ? 0.0f : (E4M3 && a.v_scale ? a.v_scale[h] : 1.0f) / l_run;
-    bf16_t* o = out + (qrow * a.hpr + head) * PHD;
-#pragma unroll
-    for (int dt = 0; dt < PHD / 32; ++dt)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        uint2 w;
-        w.x = pack2bf(oacc[dt][k * 4 + 0] * inv, oacc[dt][k * 4 + 1] * inv);
-        w.y = pack2bf(oacc[dt][k * 4 + 2] * inv, oacc[dt][k * 4 + 3] * inv);
-        *reinterpret_cast<uint2*>(o + dt * 32 + k * 8 + hf * 4) = w;
+    // ---- the next tile
+    if (!LINE || x1 <= end) break;
+    x = end;
+    if (++tile == sq.tiles) {
+      tile = 0;
+      if (++h == heads) {
+        h = 0;
+        base += heads * sq.before(sq.tiles);
+        unit0 += heads * sq.tiles;
+        do {
+          if (++b >= a.batch) return;
+          sq = load_seq(b);                        // (all lanes the same)
+          sq = pick(sq, 0);
+        } while (sq.tiles == 0);
       }
-  }
-  // ---- the next tile
-  if (!LINE || x1 <= end) break;
-  x = end;
-  if (++tile == sq.tiles) {
-    tile = 0;
-    if (++h == heads) {
-      h = 0;
-      base += heads * sq.before(sq.tiles);
-      unit0 += heads * sq.tiles;
-      do {
-        if (++b >= a.batch) return;
-        sq = load_seq(b);                        // (all lanes the same)
-        sq = pick(sq, 0);
-      } while (sq.tiles == 0);
     }
-  }
   }
 }
 

@@ -89,6 +89,27 @@ def test_the_same_bits_every_time(T, heads, kv, e4m3):
     P.check_attn(c, first, *P.ref_attn(c), P.slack(c))
 
 
+@pytest.mark.parametrize("T,heads,kv,e4m3,keys", [(8, 32, 32, False, 700), (8, 32, 32, True, 1500), (8, 32, 32, False, 60), (4, 64, 32, True, 90)])
+def test_more_units_than_waves(T, heads, kv, e4m3, keys):
+    """More (sequence, head) pairs than the waves of a launch, with long and with short caches."""
+    lens = [keys - (37 * i) % (keys // 2) for i in range(90)]
+    c = P.make(24, T, heads, kv, lens, [1] * 90, 32, e4m3)
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
+
+
+@pytest.mark.parametrize("hint", [1, 2, 5, 30, 400])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_any_number_of_new_tokens_whatever_max_new_says(hint, e4m3):
+    """max_new chooses the kernel alone."""
+    c = P.make(25, 1, 8, 2, [700, 40, 333, 0, 5], [90, 1, 33, 0, 5], 16, e4m3)
+    c.desc.max_new = hint
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
+
+
 def test_append_far_positions_and_wide_rows():
     """Positions up to 2^24 - 1 (the angle is carried beyond fp32), rows of qkv and q wider than their heads, other base."""
     far = [2 ** 24 - 16, 1000003, 131071]

@@ -34,7 +34,7 @@ def attend(d, q=FAKE, out=FAKE, row_start=FAKE, lens=FAKE, table=FAKE, k=FAKE, v
     ("cache_type", 2, B.EINVAL), ("cache_type", -1, B.EINVAL), ("n_heads", 0, B.EINVAL), ("n_kv_heads", -1, B.EINVAL),
     ("max_pages", 0, B.EINVAL), ("page_size", 0, B.EINVAL), ("head_dim", 0, B.EINVAL),
     ("T", 3, B.ESHAPE), ("n_kv_heads", 3, B.ESHAPE), ("n_kv_heads", 1, B.ESHAPE), ("head_dim", 64, B.EUNSUPPORTED),
-    ("page_size", 8, B.ESHAPE), ("page_size", 24, B.ESHAPE), ("n_pages", 1 << 31, B.ESHAPE), ("rows", 1 << 31, B.ESHAPE),
+    ("page_size", 8, B.ESHAPE), ("page_size", 24, B.ESHAPE), ("n_pages", 1 << 31, B.ESHAPE), ("rows", 1 << 31, B.ESHAPE), ("rows", (1 << 23) + 1, B.ESHAPE), ("batch", 1 << 21, B.ESHAPE),
     ("max_pages", 1 << 28, B.ESHAPE), ("n_heads", 1 << 20, B.ESHAPE),
     ("ld_q", 4 * 128 - 8, B.ESHAPE), ("ld_q", 4 * 128 + 4, B.ESHAPE), ("ld_qkv", 4 * 128, B.ESHAPE), ("ld_qkv", 8 * 128 + 1, B.ESHAPE),
     ("strides", (1 << 20, 1 << 12, 2048, 120), B.ESHAPE), ("strides", (1 << 20, 1 << 12, 2048, 64), B.ESHAPE),
