@@ -56,8 +56,14 @@ struct PromptSeq {                               // a sequence's tiles (of one r
   __device__ __forceinline__ int before(int t) const { return t * (PSTART + nb0 * 16) + slope * (t * (t - 1) / 2); }
 };
 
+// Swizzles of the 16-byte chunks of a tile's row: K is read 32 rows x one chunk at a time, V by the transpose read, 4 rows x 64
+// bytes.  Both repeat every 8 rows for V and 16 for K, which the reads' immediate offsets count on.  The e4m3 kernel writes its tiles
+// 16 rows x one chunk at a time, from rows of its buffer that are swizzled for that (pr_swz).
 __device__ __forceinline__ int pk_swz(int row, int c) { return c ^ (row & 15); }
-__device__ __forceinline__ int pv_swz(int row, int c) { return c ^ ((row & 3) << 2); }
+template <bool E4M3> __device__ __forceinline__ int pv_swz(int row, int c) {
+  return c ^ ((row & 3) << 2) ^ (E4M3 ? (row >> 2) & 1 : 0);
+}
+__device__ __forceinline__ int pr_swz(int row, int c) { return c ^ ((row >> 1) & 7); }
 // the scores are MFMA results or -inf: a signalling input needs no quieting
 __device__ __forceinline__ float pmax3(float a, float b, float c) {
   float d;
@@ -304,12 +310,13 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
     // ---- global -> LDS.  bf16: a copy fills 4 rows, the wave's rows 4 wave .. + 3 of each of the 4 groups.  e4m3: a copy fills 8 rows,
     // a wave takes the group of its number, K and V.
     const unsigned row_bytes = (unsigned)(a.s_row * ELT);
-    unsigned dko, dvo, dro = 0;
+    unsigned dko, dvo, dro[2] = {0, 0};
     {
       const int row = wave * 4 + (lane >> 4), phys = lane & 15;
       dko = row * row_bytes + pk_swz(row, phys) * 16;       // (the swizzles repeat every 16 rows)
-      dvo = row * row_bytes + pv_swz(row, phys) * 16;
-      if (E4M3) dro = (lane >> 3) * row_bytes + (lane & 7) * 16;
+      dvo = row * row_bytes + pv_swz<E4M3>(row, phys) * 16;
+      if (E4M3)
+        for (int i = 0; i < 2; ++i) dro[i] = (i * 8 + (lane >> 3)) * row_bytes + pr_swz(i * 8 + (lane >> 3), lane & 7) * 16;
     }
     auto issue_rows = [&](const unsigned char* base, unsigned off, const Place& p, int blk, uint4* t) {
       uint4* to = t + wave * 4 * PCH;
@@ -329,14 +336,14 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
       const i32x4_t rs = make_rsrc(base + p.at[0]);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        dma16(rs, i * 8 + (lane >> 3) < left ? dro + i * 8 * row_bytes : 0x80000000u, t + i * 64);
+        dma16(rs, i * 8 + (lane >> 3) < left ? dro[i] : 0x80000000u, t + i * 64);
     };
-    // the wave's group of a raw block as bf16 rows of the tile: lane = row (lane / 4) and a quarter of it
+    // the wave's group of a raw block as bf16 rows of the tile: a lane takes a quarter of a row
     auto widen = [&](const uint4* src, uint4* tile_at, bool is_v) {
-      const int r = lane >> 2, part = lane & 3, row = wave * 16 + r;
+      const int r = lane & 15, part = lane >> 4, row = wave * 16 + r;
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        const uint4 w = src[r * 8 + part * 2 + c];
+        const uint4 w = src[r * 8 + pr_swz(r, part * 2 + c)];
         const unsigned x[4] = {w.x, w.y, w.z, w.w};
         unsigned y[8];
 #pragma unroll
@@ -347,7 +354,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int ch = part * 4 + c * 2 + i;
-          tile_at[row * PCH + (is_v ? pv_swz(row, ch) : pk_swz(row, ch))] = make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+          tile_at[row * PCH + (is_v ? pv_swz<E4M3>(row, ch) : pk_swz(row, ch))] = make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
         }
       }
     };
@@ -369,7 +376,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
 #pragma unroll
       for (int dt = 0; dt < PHD / 32; ++dt) {
         const int col = dt * 32 + half * 16 + (i16 & 3) * 4;
-        voff[dt] = lds0 + ((vrow * PCH + pv_swz(vrow, col >> 3)) * 16 + (col & 7) * 2);
+        voff[dt] = lds0 + ((vrow * PCH + pv_swz<E4M3>(vrow, col >> 3)) * 16 + (col & 7) * 2);
       }
     }
     const f32x16_t zero16 = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
