@@ -509,51 +509,51 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
     };
 
     if (nblk > 0) {
-      // prologue: K(0) alone first (its scores open the pipeline), then what the first loop iteration expects
+      // prologue: what the first iteration expects is on its way at once; the scores of block 0 wait for K(0) alone
       f32x16_t sa[PBK / 32], sb[PBK / 32];
       fetch();
+      // The compiler's wait for q stands here, under the table's way and in front of the copies, which it does not know of and would
+      // wait for as well
+#pragma unroll
+      for (int ks = 0; ks < PHD / 16; ++ks) asm volatile("" : "+v"(qf[ks]));
       pk = place();
       fetch();
+      have = have_next = pk.have;
       if constexpr (E4M3) {
+        uint4* k1 = vslot(1) + wave * 128;         // K(1) lands where V(1) will be widened to
         issue_raw(kh, pk, 0, raw);
         issue_raw(vh, pk, 0, raw + 128);
-        const unsigned have0 = pk.have;
-        wait_vmcnt<0>();
-        widen(raw, kslot(0), false);
-        widen(raw + 128, vslot(0), true);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        have = have0;
         if (1 < nblk) {
           pk = place();
           fetch();
-          issue_raw(kh, pk, 1, raw);
-          issue_raw(vh, pk, 1, raw + 128);
-          wait_vmcnt<0>();
-          widen(raw, kslot(1), false);             // V(1) stays in the buffer for the first iteration
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           have_next = pk.have;
-          if (2 < nblk) {
-            pk = place();
-            fetch();
-            issue_raw(kh, pk, 2, raw);
-          }
+          issue_raw(kh, pk, 1, k1);
         }
-        __syncthreads();
+        wait_vmcnt<0>();
+        widen(raw, kslot(0), false);
+        widen(raw + 128, vslot(0), true);
+        if (1 < nblk) widen(k1, kslot(1), false);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (1 < nblk) issue_raw(vh, pk, 1, raw + 128);   // V(1) stays in the buffer for the first iteration
+        if (2 < nblk) {
+          pk = place();
+          fetch();
+          issue_raw(kh, pk, 2, raw);
+        }
       } else {
         issue_rows(kh, dko, pk, 0, kslot(0));
-        wait_vmcnt<0>();
-        __syncthreads();
-        have = pk.have;
         issue_rows(vh, dvo, pk, 0, vslot(0));
         if (1 < nblk) {
           pk = place();
           fetch();
+          have_next = pk.have;
           issue_rows(kh, dko, pk, 1, kslot(1));
+          wait_vmcnt<8>();
+        } else {
+          wait_vmcnt<4>();
         }
-        have_next = pk.have;
       }
-#pragma unroll
-      for (int ks = 0; ks < PHD / 16; ++ks) asm volatile("" : "+v"(qf[ks]));   // the compiler's wait for q stands in front of the loop
+      __syncthreads();
 #pragma unroll
       for (int j = 0; j < PBK / 32; ++j)
 #pragma unroll
