@@ -659,10 +659,13 @@ hipError_t launch_paged_few(const PagedArgs& a, int e4m3, int max_new, const bf1
   const long long kb = e4m3 ? 32 : 16, nb = (cap + kb - 1) / kb;
   const int nt = few_tiles(a, max_new);
   const long long units = few_units(a, nt);
-  // A cache of so few keys that a wave does them in the time of a second kernel's launch, then one of so few that a workgroup
-  // does (and the launch has one for every unit)
-  const int mode = nb <= 4 ? FEW_WAVE : nb <= 8 * FNW && units <= FMAX_WGS ? FEW_WG : FEW_LINE;
-  const int least = mode == FEW_LINE ? 2 : 1;
+  // A cache (as wide as its table) of so few keys that a workgroup does them in the time of a second kernel's launch, while the launch
+  // has one for every unit; one of so few that a wave does.  In us, 32 heads, bf16: one sequence of 300 keys 13.2 in the line, 9.1
+  // a workgroup each; 128 sequences of 60 keys 28.1 in the line, 26.1 a wave each, of 120 keys 45.7 and 43.6; one sequence of 60
+  // keys 8.6 a wave each, 7.6 a workgroup.  Two tiles take a workgroup's joins longer: 31 sequences of 14 keys, 32 rows each, 8.6 a
+  // wave each, 11.9 a workgroup, of 120 keys 17.0 and 14.9.
+  const int mode = nb <= 4 && nt > 1 ? FEW_WAVE : nb <= 8 * FNW && units <= FMAX_WGS ? FEW_WG : nb <= 8 ? FEW_WAVE : FEW_LINE;
+  const int least = mode == FEW_LINE ? 2 : 1;    // both slots of a wave (one of 3001 keys, 64 / 8 heads, 1 / 2 / 4 blocks: 16.0 / 13.7 / 15.0 us)
   const long long most = mode == FEW_WG ? units * FNW : mode == FEW_WAVE ? units : units * (nb + FSTART * FNW);
   const int wgs = (int)std::min<long long>(FMAX_WGS, (most + least * FNW - 1) / (least * FNW));
   const int unit_joins = mode == FEW_LINE && units <= FMAX_WGS * FNW ? (int)units : 0;

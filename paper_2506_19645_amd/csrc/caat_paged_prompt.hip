@@ -35,11 +35,14 @@ static constexpr int PRAW = 4 * 256;             // chunks of the waves' e4m3 bu
 static constexpr int PPR = PHD + 4;              // floats of a partial row: 128 sums, maximum, denominator, 2 unused
 static constexpr int PWGS = 512;                 // workgroups that run at a time
 
-// Few tiles (at most PLINE, of all heads) do not fill the chip, or fill it unevenly: then the tiles of all sequences stand in one
-// line, each as long as its blocks and PSTART more (its start and its results' way), and every workgroup takes an equal stretch.
-// Places count sixteenths of a block; a tile's length is taken as linear in its number, nb0 blocks the first to nb0 + slope / 16 *
+// Few tiles (at most PLINE, of all heads) over many keys do not fill the chip, or fill it unevenly: then the tiles of all sequences
+// stand in one line, each as long as its blocks and PSTART more (its start and its results' way), and every workgroup takes an equal
+// stretch.  In us, a tile per workgroup (few tiles: an equal share of its keys) / the line: 216 tiles of a ragged batch with up to 6000
+// keys 76 / 43, 232 with up to 5003 90 / 82, 8 over 52000 57 / 51, 256 of one prompt over 16384 320 / 323; but 520 tiles of two
+// prompts over 8192 keys 270 / 294, and 160 over 900 keys 30 / 38: the line needs PLINE_KEYS blocks of keys too.  Places count sixteenths of a block; a tile's length is taken as linear in its number, nb0 blocks the first to nb0 + slope / 16 *
 // number, which is what causality makes it up to roundings.
 static constexpr int PLINE = 384;
+static constexpr int PLINE_KEYS = 24;
 static constexpr int PSTART = 3 * 16;
 static constexpr int PLEAST = 8 * 16;            // shortest stretch
 
@@ -699,7 +702,7 @@ size_t paged_prompt_workspace_bytes(const PagedArgs& a) {
 hipError_t launch_paged_prompt(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, void* workspace,
                                hipStream_t s) {
   const long long tiles = prompt_tiles(a), most = ((long long)a.max_pages * a.page_size / PBK + 2) * 16 + PSTART;   // of a tile
-  const int line_room = tiles <= PLINE && most >= 24 * 16 && most <= 0x7FFFFFFFLL / tiles ? (int)tiles : 0;
+  const int line_room = tiles <= PLINE && most >= PLINE_KEYS * 16 && most <= 0x7FFFFFFFLL / tiles ? (int)tiles : 0;
   PromptJoin* joins = reinterpret_cast<PromptJoin*>(workspace);
   float* part = reinterpret_cast<float*>(joins + PLINE);
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)PHD);
@@ -709,7 +712,7 @@ hipError_t launch_paged_prompt(const PagedArgs& a, int e4m3, const bf16_t* q, bf
   hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), 0, s, a, q, out, kc, vc, part, joins, scale_log2, line_room);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !line_room) return e;
-  if (tiles <= PWGS / 8)                         // many parts of a tile
+  if (tiles <= PWGS / 8)                         // many parts of a tile (8 tiles over 52000 keys 82 -> 66 us, 64 over 16384: 79 and 78)
     hipLaunchKernelGGL(paged_prompt_join_kernel<8>, dim3((unsigned)tiles, PBQ), dim3(256), 0, s, a, part, joins, out);
   else
     hipLaunchKernelGGL(paged_prompt_join_kernel<1>, dim3((unsigned)tiles, PBQ / 8), dim3(256), 0, s, a, part, joins, out);
