@@ -283,8 +283,9 @@ int caat_block_bwd(const caat_desc* d, const void* const* weights, const void* x
  * Both, and the table, are read on the device, so a captured call follows them from replay to replay.  What they hold is
  * checked there: a sequence whose rows are not inside 0 .. rows (or end before they begin) has none, a negative length is
  * none, a table entry outside 0 .. n_pages - 1, or a position at or behind max_pages * page_size, is no page: nothing is
- * written there, and its keys are not seen.  A page may stand in the tables of several sequences (a common beginning);
- * two tokens of one call must not be appended to the same place.  Rows that belong to no sequence are left as they are.
+ * written there, and its keys are not seen.  A page may stand in the tables of several sequences (a common beginning), but
+ * no row may belong to two sequences, nor two tokens of one call be appended to the same place: what such rows and
+ * places get is undefined.  Rows that belong to no sequence are left as they are.
  */
 typedef enum caat_cache {
   CAAT_CACHE_BF16 = 0,
@@ -326,7 +327,7 @@ int caat_paged_append(const caat_paged_desc* d, const void* qkv, void* q_out, co
 /*
  * Causal attention of the new tokens over the pages of their sequences (their own keys are read from the cache, so they are
  * appended first): out[row of token i of b, head] = sum_t softmax_t(q . k_t / sqrt(128)) v_t over positions
- * t <= lens[b] - n + i.  q [T, rows, hd_r] with rotated queries, out [T, rows, hd_r] packed.  A row that sees no key, or whose
+ * t <= lens[b] - n + i.  q [T, rows, hd_r] with rotated queries, out [T, rows, hd_r] packed, which must not overlap q.  A row that sees no key, or whose
  * scores are all minus infinity, is zeros.  Nothing that lies in a page behind its sequence's length takes part, whatever it
  * holds.  workspace: caat_paged_attn_workspace_bytes(d) bytes, which depends neither on the lengths nor on max_pages;
  * nothing in it has to be kept or cleared between calls.

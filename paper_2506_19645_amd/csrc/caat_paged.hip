@@ -5,9 +5,30 @@
 
 namespace caat {
 
-// The sequence that owns a row (the first one, -1: none); called by whole waves, the answer is uniform.
+// The sequence that owns a row (-1: none); called by whole waves, the answer is uniform.  Among many sequences the last one whose
+// rows begin at or before the row is found 64 at a time; if the list does not run upwards, and so that one does not own the row,
+// they are gone through.
 __device__ __forceinline__ int seq_of_row(const PagedArgs& a, int row, int& first, int& n) {
   const int lane = threadIdx.x & 63;
+  if (!a.row_start) {
+    first = row;
+    n = 1;
+    return row < a.batch ? row : -1;
+  }
+  if (a.batch > 64) {
+    int lo = 0, size = a.batch;                  // among lo .. lo + size - 1
+    while (size > 1) {
+      const int step = (size + 63) / 64, at = lane * step;
+      const bool before = at < size && a.row_start[lo + at] <= row;
+      const int k = __popcll(__ballot(before));  // (lane 0 .. k - 1, if the list runs upwards)
+      if (k == 0) break;
+      lo += (k - 1) * step;
+      size = min(step, size - (k - 1) * step);
+    }
+    lo = uni(lo);
+    n = seq_rows(a, lo, first);
+    if (n > 0 && row >= first && row < first + n) return lo;
+  }
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     int f = 0, m = 0;
     if (b0 + lane < a.batch) m = seq_rows(a, b0 + lane, f);

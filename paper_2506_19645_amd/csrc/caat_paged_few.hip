@@ -95,24 +95,32 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
   auto load_seqs = [&](int at, int start_blocks) {
     SeqChunk c;
     c.at = at;
-    c.first = c.n = c.len = c.units = 0;
-    c.work = 0;
-    if (at + lane < a.batch) {
-      c.n = seq_rows(a, at + lane, c.first);
-      c.len = max(a.lens[at + lane], 0);
-      const int nb = mode == FEW_LINE ? (min(c.len, cap) + KB - 1) / KB + start_blocks : 1;
-      c.units = (int)(((long long)c.n * grp + ROWS - 1) / ROWS);
-      c.work = c.units * nb;
-    }
+    const int b = min(at + lane, a.batch - 1);   // (no branch: several chunks' loads are under way at once)
+    c.n = at + lane < a.batch ? seq_rows(a, b, c.first) : 0;
+    c.len = max(a.lens[b], 0);
+    const int nb = mode == FEW_LINE ? (min(c.len, cap) + KB - 1) / KB + start_blocks : 1;
+    c.units = (int)(((long long)c.n * grp + ROWS - 1) / ROWS);
+    c.work = c.units * nb;
     return c;
   };
   SeqChunk sq = load_seqs(0, 0);
   int units_to = wave_sums(sq.units), work_to = wave_sums(sq.work);
   int units = __builtin_amdgcn_readlane(units_to, 63), total = __builtin_amdgcn_readlane(work_to, 63);
-  for (int at = 64; at < a.batch; at += 64) {
-    const SeqChunk c = load_seqs(at, 0);
-    units += __builtin_amdgcn_readlane(wave_sums(c.units), 63);
-    total += __builtin_amdgcn_readlane(wave_sums(c.work), 63);
+  int chunk_units = lane ? 0 : units, chunk_work = lane ? 0 : total;   // lane k: of chunk k, the first 64 of them
+  for (int at = 64; at < a.batch; at += 256) {
+    SeqChunk c[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) c[k] = load_seqs(at + 64 * k, 0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int u = __builtin_amdgcn_readlane(wave_sums(c[k].units), 63), w = __builtin_amdgcn_readlane(wave_sums(c[k].work), 63);
+      units += u;
+      total += w;
+      if (lane == at / 64 + k) {
+        chunk_units = u;
+        chunk_work = w;
+      }
+    }
   }
   units *= heads;                                // (the host has checked that the line has less than 2^31 places)
   total *= heads;
@@ -130,6 +138,18 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
     // many sequences can make the line longer than 31 bits, and what stands here wrong: the checks that follow keep
     // such a wave inside the buffers.)
     int b = a.batch, unit0 = 0, base = 0;
+    if (a.batch > 64) {                          // its chunk, or the last of the first 64
+      const int own = chunk_work + chunk_units * start_blocks, upto = wave_sums(own), uupto = wave_sums(chunk_units);
+      const unsigned long long over = __ballot(upto * heads > x0);
+      const int k = over ? __builtin_ctzll(over) : 63;
+      if (k > 0) {
+        base = __builtin_amdgcn_readlane(upto - own, k) * heads;
+        unit0 = __builtin_amdgcn_readlane(uupto - chunk_units, k) * heads;
+        sq = load_seqs(64 * k, start_blocks);
+        work_to = wave_sums(sq.work);
+        units_to = wave_sums(sq.units);
+      }
+    }
     while (sq.at < a.batch) {
       const unsigned long long over = __ballot(base + work_to * heads > x0);
       if (over) {

@@ -112,10 +112,10 @@ def ref_attn(c, q=None, k=None, v=None):
     out = np.full((c.T, c.rows, c.hpr * D), np.nan)
     size = np.zeros_like(out)
     grp = c.hpr // c.kvpr
-    for b in range(len(c.news)):
-        here = [(row, pos) for bb, row, pos in _tokens(c) if bb == b]
-        if not here:
-            continue
+    owned = {}
+    for b, row, pos in _tokens(c):
+        owned.setdefault(b, []).append((row, pos))
+    for b, here in owned.items():
         last = min(here[-1][1] + 1, c.table.shape[1] * c.page)
         spots = [(t, _page(c, b, t)) for t in range(last)]
         spots = [(t, g) for t, g in spots if g >= 0]

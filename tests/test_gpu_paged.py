@@ -99,6 +99,46 @@ def test_more_units_than_waves(T, heads, kv, e4m3, keys):
     P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
 
 
+@pytest.mark.parametrize("batch", [65, 300, 4300])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_many_sequences(batch, e4m3):
+    """More sequences than a wave looks at together, and than it keeps sums of; free slots among them."""
+    lens = [(7 * i) % 61 for i in range(batch)]
+    lens[batch - 2] = 500
+    c = P.make(26, 1, 2, 1, lens, [int(x > 0 and i % 7 != 3) for i, x in enumerate(lens)], 16, e4m3)
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
+    P.append(c, d)
+    P.check_append(c, P.bits(d.q_out), P.bits(d.k), P.bits(d.v), c.k, c.v)
+
+
+@pytest.mark.parametrize("batch", [5, 90])
+def test_rows_in_another_order_than_the_sequences(batch):
+    """Sequence 0 owns the last rows, sequence 2 the first ones; nobody owns any other way."""
+    news = [30, 0, 50] + [0] * (batch - 3)
+    c = P.make(27, 1, 4, 2, [77, 5, 50] + [9] * (batch - 3), news, 16)
+    c.row_start = np.array([50, 80, 0] + [50] * (batch - 2), dtype=np.int32)
+    d = P.on_gpu(c)
+    P.append(c, d)
+    P.check_append(c, P.bits(d.q_out), P.bits(d.k), P.bits(d.v), c.k, c.v)
+    P.attend(c, d, q=d.q_out)
+    c.k, c.v = P.bits(d.k), P.bits(d.v)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c, q=P.bits(d.q_out)), P.slack(c))
+
+
+def test_the_caches_own_order_without_strides():
+    """Strides of 0: [rank][page][head][position][channel], the same bits as with the strides spelled out."""
+    c = P.make(28, 2, 8, 4, [100, 33], [1, 1], 48)
+    d, e = P.on_gpu(c), P.on_gpu(c)
+    P.append(c, d)
+    P.attend(c, d, q=d.q_out)
+    c.desc.stride_rank = c.desc.stride_page = c.desc.stride_head = c.desc.stride_row = 0
+    P.append(c, e)
+    P.attend(c, e, q=e.q_out)
+    assert all(np.array_equal(P.bits(getattr(d, x)), P.bits(getattr(e, x))) for x in ("q_out", "k", "v", "out"))
+
+
 @pytest.mark.parametrize("hint", [1, 2, 5, 30, 400])
 @pytest.mark.parametrize("e4m3", [False, True])
 def test_any_number_of_new_tokens_whatever_max_new_says(hint, e4m3):
