@@ -42,8 +42,8 @@ bool paged_few_takes(const PagedArgs& a, int max_new);
 size_t paged_few_workspace_bytes(const PagedArgs& a, int max_new);
 hipError_t launch_paged_few(const PagedArgs& a, int e4m3, int max_new, const bf16_t* q, bf16_t* out, const void* kc, const void* vc,
                             void* workspace, hipStream_t s);
-size_t paged_prompt_workspace_bytes(const PagedArgs& a);
-hipError_t launch_paged_prompt(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, void* workspace,
-                               hipStream_t s);
+size_t paged_prompt_workspace_bytes(const PagedArgs& a, int max_new);
+hipError_t launch_paged_prompt(const PagedArgs& a, int e4m3, int max_new, const bf16_t* q, bf16_t* out, const void* kc, const void* vc,
+                               void* workspace, hipStream_t s);
 
 }  // namespace caat

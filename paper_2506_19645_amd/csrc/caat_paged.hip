@@ -172,13 +172,13 @@ hipError_t launch_paged_append(const PagedArgs& a, int e4m3, const bf16_t* qkv, 
 }
 
 size_t paged_attn_workspace_bytes(const PagedArgs& a, int max_new) {
-  return paged_few_takes(a, max_new) ? paged_few_workspace_bytes(a, max_new) : paged_prompt_workspace_bytes(a);
+  return paged_few_takes(a, max_new) ? paged_few_workspace_bytes(a, max_new) : paged_prompt_workspace_bytes(a, max_new);
 }
 
 hipError_t launch_paged_attn(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, int max_new,
                              void* workspace, hipStream_t s) {
   if (paged_few_takes(a, max_new)) return launch_paged_few(a, e4m3, max_new, q, out, kc, vc, workspace, s);
-  return launch_paged_prompt(a, e4m3, q, out, kc, vc, workspace, s);
+  return launch_paged_prompt(a, e4m3, max_new, q, out, kc, vc, workspace, s);
 }
 
 }  // namespace caat

@@ -2,7 +2,8 @@
 //
 // What bounds it: the two products' MFMAs and the vector work per score beside them.  A workgroup of 4 waves owns 128 consecutive
 // (token, query head of the group) rows of one sequence, rank and key / value head, so grouped heads share the rows of K
-// and V; a wave owns 32 of them and walks the keys in blocks of 64 with an online softmax.  Scores are computed transposed
+// and V; a wave owns 32 of them and walks the keys in blocks of 64 with an online softmax.  (Where no sequence is said to have more
+// than 64 rows, a workgroup owns 64 and two waves share 32 of them.)  Scores are computed transposed
 // (S^T = K q^T, 32x32x16 MFMAs), so that a lane owns one query row and the exponentiated score registers, rounded to bf16, are the
 // k-slices of the second product; V comes through the LDS transpose read.  The body is software-pipelined inside a wave: the
 // score MFMAs of block b + 1 are issued one per step between the softmax arithmetic of block b.
@@ -27,7 +28,6 @@ typedef __attribute__((address_space(3))) short4_t* lds_s4_t;
 typedef __attribute__((address_space(4))) const int* const_i_t;
 typedef __attribute__((address_space(4))) const char* const_c_t;
 
-static constexpr int PBQ = 128;                  // query rows per workgroup (32 per wave)
 static constexpr int PBK = 64;                   // keys per block
 static constexpr int PCH = PHD / 8;              // 16-byte chunks per row of a tile
 static constexpr int PTILE = PBK * PCH;          // chunks of a tile
@@ -39,7 +39,8 @@ static constexpr int PWGS = 512;                 // workgroups that run at a tim
 // stand in one line, each as long as its blocks and PSTART more (its start and its results' way), and every workgroup takes an equal
 // stretch.  In us, a tile per workgroup (few tiles: an equal share of its keys) / the line: 216 tiles of a ragged batch with up to 6000
 // keys 76 / 43, 232 with up to 5003 90 / 82, 8 over 52000 57 / 51, 256 of one prompt over 16384 320 / 323; but 520 tiles of two
-// prompts over 8192 keys 270 / 294, and 160 over 900 keys 30 / 38: the line needs PLINE_KEYS blocks of keys too.  Places count sixteenths of a block; a tile's length is taken as linear in its number, nb0 blocks the first to nb0 + slope / 16 *
+// prompts over 8192 keys 270 / 294, and 160 over 900 keys 30 / 38: the line needs PLINE_KEYS blocks of keys too.
+// Places count sixteenths of a block; a tile's length is taken as linear in its number, nb0 blocks the first to nb0 + slope / 16 *
 // number, which is what causality makes it up to roundings.
 static constexpr int PLINE = 384;
 static constexpr int PLINE_KEYS = 24;
@@ -75,22 +76,29 @@ __device__ __forceinline__ float pmax3(float a, float b, float c) {
 }
 
 // LINE: the workgroup takes a stretch of the line (line_room: tiles that joins has room for), otherwise one tile
-template <bool E4M3, bool LINE>
+// RG: groups of 32 query rows of a tile.  4: a wave owns a group.  2: two waves share a group, each takes half of every block's keys,
+// and their results meet in LDS; for sequences with at most 64 rows, of which two waves of a tile of 128 would have none (64 heads on
+// 8 ranks, 8 key / value heads, 5 new tokens; tiles of 128 / 64 rows in us: 4 sequences over 6000 keys 38.7 / 33.8, e4m3 39.2 / 30.6,
+// 24 over 6000 151 / 131, e4m3 118 / 92, 64 over 500 32.3 / 31.6; 8 new tokens 157 / 137 and 122 / 95 of the 24).
+template <bool E4M3, bool LINE, int RG>
 __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a, const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
                                                               const void* __restrict__ kc, const void* __restrict__ vc,
                                                               float* __restrict__ part, PromptJoin* __restrict__ joins, float scale_log2,
                                                               int line_room) {
   constexpr int ELT = E4M3 ? 1 : 2;
+  constexpr int BQ = 32 * RG;                    // query rows of a tile
+  constexpr int KT = RG / 2;                     // tiles of 32 keys of a block that are a wave's
   __shared__ uint4 smem[4 * PTILE + (E4M3 ? PRAW : 0)];   // K slots 0 and 1, V slots 0 and 1, 16 KB each; e4m3 buffers
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = uni(tid >> 6);
   const int frow = lane & 31, hf = lane >> 5;
+  const int rg = wave % RG, part_of = wave / RG;  // group of rows, half of the keys (0 where there is one)
   const int grp = a.hpr / a.kvpr, heads = a.T * a.kvpr;
 
   const int cap = a.max_pages * a.page_size;
   // blocks of keys that a tile's rows see; a token t of n sees those below len - n + t + 1
   auto tile_end = [&](int n, int len, int t) {   // may be 0 or less
-    const int last_token = min(n - 1, (int)(((long long)t * PBQ + PBQ - 1) / grp));
+    const int last_token = min(n - 1, (int)(((long long)t * BQ + BQ - 1) / grp));
     return min(min(len, cap), len - n + last_token + 1);
   };
   auto load_seq = [&](int b) {
@@ -99,7 +107,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
     if (b < a.batch) {
       q.n = seq_rows(a, b, q.first);
       q.len = max(a.lens[b], 0);
-      q.tiles = (int)(((long long)q.n * grp + PBQ - 1) / PBQ);
+      q.tiles = (int)(((long long)q.n * grp + BQ - 1) / BQ);
       if (LINE && q.tiles > 0) {
         q.nb0 = max(1, (tile_end(q.n, q.len, 0) + PBK - 1) / PBK);
         const int nbl = max(q.nb0, (tile_end(q.n, q.len, q.tiles - 1) + PBK - 1) / PBK);
@@ -185,7 +193,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
     const int n = sq.n, first = sq.first, len = sq.len;
     const int rank = h / a.kvpr, kvh = h - rank * a.kvpr;
     const int keys = min(len, cap);
-    const int row0 = tile * PBQ;
+    const int row0 = tile * BQ;
     const int kv_end = tile_end(n, len, tile);     // may be 0 or less
     const int all_blk = max(0, (kv_end + PBK - 1) / PBK);
     // its blocks that are this workgroup's: blk0 .. blk0 + nblk - 1
@@ -204,12 +212,12 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
     if (LINE && more) __syncthreads();                     // everyone is done with the last tile's blocks
 
     // ---- Q fragments: B operand of S^T = K q^T: lane (row frow, k-half hf) holds q[16 ks + 8 hf .. + 7]
-    const int qr = row0 + wave * 32 + frow;
+    const int qr = row0 + rg * 32 + frow;
     const int token = qr / grp, head = kvh * grp + (qr - token * grp);
     const bool row_ok = token < n;
     const long long qrow = (long long)rank * a.rows + first + token;
     const int lim = row_ok ? (int)min((long long)len - n + token + 1, (long long)keys) : kv_end;
-    const int wave_lim = uni((int)min((long long)len - n + (row0 + wave * 32) / grp + 1, (long long)keys));   // of the wave's first row
+    const int wave_lim = uni((int)min((long long)len - n + (row0 + rg * 32) / grp + 1, (long long)keys));   // of the wave's first row
     bf16x8_t qf[PHD / 16];
     const bf16_t* src = q + (row_ok ? qrow * a.ld_q + head * PHD : 0) + hf * 8;   // rows of nobody: any row, not stored
 #pragma unroll
@@ -373,13 +381,13 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
     {
       const lds_c_t lds0 = (lds_c_t)smem;
 #pragma unroll
-      for (int ks = 0; ks < PHD / 16; ++ks) koff[ks] = (lds_u4_t)(lds0 + (frow * PCH + pk_swz(frow, ks * 2 + hf)) * 16);
+      for (int ks = 0; ks < PHD / 16; ++ks) koff[ks] = (lds_u4_t)(lds0 + ((part_of * 32 + frow) * PCH + pk_swz(frow, ks * 2 + hf)) * 16);
       const int i16 = lane & 15, half = (lane >> 4) & 1;
       const int vrow = 4 * hf + (i16 >> 2);
 #pragma unroll
       for (int dt = 0; dt < PHD / 32; ++dt) {
         const int col = dt * 32 + half * 16 + (i16 & 3) * 4;
-        voff[dt] = lds0 + ((vrow * PCH + pv_swz<E4M3>(vrow, col >> 3)) * 16 + (col & 7) * 2);
+        voff[dt] = lds0 + (((part_of * 32 + vrow) * PCH + pv_swz<E4M3>(vrow, col >> 3)) * 16 + (col & 7) * 2);
       }
     }
     const f32x16_t zero16 = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
@@ -416,20 +424,20 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
         if (blk + 1 < nblk) issue_rows(vh, dvo, pv, blk + 1, vslot(blk + 1));
       }
       const int kv0 = key0 + blk * PBK;
-      // ---- mask (keys of register r: kv0 + 32 j + 8 (r / 4) + 4 hf + r % 4): only where some row of the wave does not see the whole
-      // block, or a group has no page
+      // ---- mask (keys of register r: kv0 + 32 (part_of + j) + 8 (r / 4) + 4 hf + r % 4): only where some row of the wave does not see
+      // the whole block, or a group has no page
       if (kv0 + PBK > wave_lim || have != 15u) {
 #pragma unroll
-        for (int j = 0; j < PBK / 32; ++j)
+        for (int j = 0; j < KT; ++j)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const int key = kv0 + j * 32 + 8 * (r >> 2) + 4 * hf + (r & 3);
-            if (key >= lim || !(have >> (j * 2 + (r >> 3)) & 1)) scur[j][r] = -INFINITY;
+            const int key = kv0 + (part_of + j) * 32 + 8 * (r >> 2) + 4 * hf + (r & 3);
+            if (key >= lim || !(have >> ((part_of + j) * 2 + (r >> 3)) & 1)) scur[j][r] = -INFINITY;
           }
       }
       have = have_next;
       have_next = E4M3 ? pv.have : pk.have;
-      // ---- one MFMA per step, a scheduling fence behind each:
+      // ---- one MFMA per step, a scheduling fence behind each (64 keys; of 32 half as many):
       //   steps 0-15 : score MFMAs of block blk + 1 (fragments read three steps ahead); underneath: the row maximum (steps 0-3),
       //                its exchange with the other half-row (4-5), the exponentials of keys 0-31 (6-13)
       //   steps 16-31: second-product MFMAs; underneath: the exponentials of keys 32-63 (steps 16-23)
@@ -437,7 +445,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
       auto kread = [&](int idx) -> u32x4_t { return koff[idx & 7][((SLOT ^ 1) * TILE_BYTES + (idx >> 3) * 32 * PCH * 16) / 16]; };
       __builtin_amdgcn_s_setprio(1);               // in front of a wave that waits for its copies (e4m3 chunk 332 -> 320 us, others even)
       float mx = -INFINITY, mxo = 0.0f, m_new = 0.0f, alpha = 1.0f, mb = 0.0f, psum = 0.0f;
-      unsigned pw[PBK / 2];                        // the block's probabilities, bf16 pairs
+      unsigned pw[8 * KT];                         // the block's probabilities, bf16 pairs
       auto prob_pair = [&](int i) {
         const int j = i >> 3, r = (i & 7) * 2;
         const float p0 = __builtin_amdgcn_exp2f(scur[j][r] * scale_log2 - mb);
@@ -455,25 +463,25 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
       }
       fence();
 #pragma unroll
-      for (int idx = 0; idx < 16; ++idx) {
+      for (int idx = 0; idx < 8 * KT; ++idx) {
         if constexpr (!LAST) {
           const int j = idx >> 3, ks = idx & 7;
           const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, kr[idx % 3]);
           snext[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], ks == 0 ? zero16 : snext[j], 0, 0, 0);
-          if (idx + 3 < 16) kr[idx % 3] = kread(idx + 3);
+          if (idx + 3 < 8 * KT) kr[idx % 3] = kread(idx + 3);
         }
-        if (idx < 4) {
+        if (idx < 2 * KT) {
           const int j = idx >> 1, r0 = (idx & 1) * 8;
 #pragma unroll
           for (int r = 0; r < 8; r += 2) mx = pmax3(mx, scur[j][r0 + r], scur[j][r0 + r + 1]);
-          if (idx == 3) mxo = __shfl_xor(mx, 32, 64);
-        } else if (idx == 5) {
+          if (idx == 2 * KT - 1) mxo = __shfl_xor(mx, 32, 64);
+        } else if (idx == 2 * KT + 1) {
           m_new = fmaxf(m_run, fmaxf(mx, mxo));
           const float mz = m_new == -INFINITY ? 0.0f : m_new;   // no key seen so far: nothing is added
           alpha = __builtin_amdgcn_exp2f((m_run - mz) * scale_log2);
           mb = mz * scale_log2;
-        } else if (idx >= 6 && idx < 14) {
-          prob_pair(idx - 6);
+        } else if (idx >= 2 * KT + 2 && idx < 6 * KT + 2) {
+          prob_pair(idx - 2 * KT - 2);
         }
         fence();
       }
@@ -497,14 +505,14 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
       vread(2, va[2], vb[2]);
       fence();
 #pragma unroll
-      for (int st = 0; st < 16; ++st) {
+      for (int st = 0; st < 8 * KT; ++st) {
         const int u = st >> 2, dt = st & 3;
         const short8_t vv = {va[st % 3][0], va[st % 3][1], va[st % 3][2], va[st % 3][3],
                              vb[st % 3][0], vb[st % 3][1], vb[st % 3][2], vb[st % 3][3]};
         const bf16x8_t pfu = __builtin_bit_cast(bf16x8_t, make_uint4(pw[4 * u], pw[4 * u + 1], pw[4 * u + 2], pw[4 * u + 3]));
         oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vv), pfu, oacc[dt], 0, 0, 0);
-        if (st + 3 < 16) vread(st + 3, va[st % 3], vb[st % 3]);
-        if (st < 8) prob_pair(8 + st);
+        if (st + 3 < 8 * KT) vread(st + 3, va[st % 3], vb[st % 3]);
+        if (st < 4 * KT) prob_pair(4 * KT + st);
         fence();
       }
       l_run = l_run * alpha + psum;
@@ -513,7 +521,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
 
     if (nblk > 0) {
       // prologue: what the first iteration expects is on its way at once; the scores of block 0 wait for K(0) alone
-      f32x16_t sa[PBK / 32], sb[PBK / 32];
+      f32x16_t sa[KT], sb[KT];
       fetch();
       // The compiler's wait for q stands here, under the table's way and in front of the copies, which it does not know of and would
       // wait for as well
@@ -558,7 +566,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
       }
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < PBK / 32; ++j)
+      for (int j = 0; j < KT; ++j)
 #pragma unroll
         for (int ks = 0; ks < PHD / 16; ++ks) {
           const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, koff[ks][(j * 32 * PCH * 16) / 16]);
@@ -579,15 +587,44 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
 
     // ---- normalise and store: lane holds out[row][32 dt + 8 (r / 4) + 4 hf + r % 4]
     l_run += __shfl_xor(l_run, 32, 64);
+    if constexpr (RG == 2) {
+      // the second halves' results through the tiles' place: 16 chunks of 4 sums per lane, then maximum and denominator
+      float4* po = reinterpret_cast<float4*>(smem) + rg * 16 * 64;
+      float2* pm = reinterpret_cast<float2*>(reinterpret_cast<float4*>(smem) + 2 * 16 * 64) + rg * 64;
+      __syncthreads();
+      if (part_of == 1) {
+#pragma unroll
+        for (int c = 0; c < 16; ++c)
+          po[c * 64 + lane] = make_float4(oacc[c >> 2][(c & 3) * 4], oacc[c >> 2][(c & 3) * 4 + 1], oacc[c >> 2][(c & 3) * 4 + 2],
+                                          oacc[c >> 2][(c & 3) * 4 + 3]);
+        pm[lane] = make_float2(m_run, l_run);
+      }
+      __syncthreads();
+      if (part_of == 0) {
+        const float2 ml = pm[lane];
+        const float m_new = fmaxf(m_run, ml.x), mz = m_new == -INFINITY ? 0.0f : m_new;
+        const float f0 = __builtin_amdgcn_exp2f((m_run - mz) * scale_log2), f1 = __builtin_amdgcn_exp2f((ml.x - mz) * scale_log2);
+        m_run = m_new;
+        l_run = l_run * f0 + ml.y * f1;
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+          const float4 o = po[c * 64 + lane];
+          const float v[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) oacc[c >> 2][(c & 3) * 4 + k] = oacc[c >> 2][(c & 3) * 4 + k] * f0 + v[k] * f1;
+        }
+      }
+    }
+    const bool stores = row_ok && part_of == 0;
     if (LINE && begins && tid == 0) {
       PromptJoin* j = joins + unit0 + h * sq.tiles + tile;
       if ((unsigned)(unit0 + h * sq.tiles + tile) < (unsigned)line_room)
-        *j = PromptJoin{all_here ? 0 : min(PBQ, n * grp - row0), rank, kvh, first, row0, begin, end, per};
+        *j = PromptJoin{all_here ? 0 : min(BQ, n * grp - row0), rank, kvh, first, row0, begin, end, per};
     }
     if (LINE && !all_here) {
       const int taker = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
-      if (row_ok) {
-        float* o = part + ((2LL * taker + (begins ? 1 : 0)) * PBQ + wave * 32 + frow) * PPR;
+      if (stores) {
+        float* o = part + ((2LL * taker + (begins ? 1 : 0)) * BQ + rg * 32 + frow) * PPR;
 #pragma unroll
         for (int dt = 0; dt < PHD / 32; ++dt)
 #pragma unroll
@@ -596,7 +633,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
                 make_float4(oacc[dt][k * 4], oacc[dt][k * 4 + 1], oacc[dt][k * 4 + 2], oacc[dt][k * 4 + 3]);
         if (hf == 0) *reinterpret_cast<float2*>(o + PHD) = make_float2(m_run * scale_log2, l_run);
       }
-    } else if (row_ok) {
+    } else if (stores) {
       const float inv = l_run == 0.0f ? 0.0f : (E4M3 && a.v_scale ? a.v_scale[h] : 1.0f) / l_run;
       bf16_t* o = out + (qrow * a.hpr + head) * PHD;
 #pragma unroll
@@ -631,7 +668,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
 // Joins the parts of a tile, in the order of the keys: 32 threads, 4 channels each, for a row and every SUBS-th part of it.
 template <int SUBS>
 __global__ __launch_bounds__(256) void paged_prompt_join_kernel(const PagedArgs a, const float* __restrict__ part,
-                                                                const PromptJoin* __restrict__ joins, bf16_t* __restrict__ out) {
+                                                                const PromptJoin* __restrict__ joins, bf16_t* __restrict__ out, int bq) {
   __shared__ float4 s_num[SUBS > 1 ? 256 : 1];
   __shared__ float2 s_ml[SUBS];
   const PromptJoin j = joins[blockIdx.x];
@@ -646,7 +683,7 @@ __global__ __launch_bounds__(256) void paged_prompt_join_kernel(const PagedArgs 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int k = min(p0 + i * SUBS, parts - 1);
-      const float* q = part + ((2LL * (w0 + k) + (k == 0 ? 1 : 0)) * PBQ + r) * PPR;   // the first one's lies behind that of the tile before
+      const float* q = part + ((2LL * (w0 + k) + (k == 0 ? 1 : 0)) * bq + r) * PPR;   // the first one's lies behind that of the tile before
       ml[i] = *reinterpret_cast<const float2*>(q + PHD);
       v[i] = *reinterpret_cast<const float4*>(q + c);
       if (p0 + i * SUBS >= parts) ml[i].x = -INFINITY;
@@ -689,33 +726,43 @@ __global__ __launch_bounds__(256) void paged_prompt_join_kernel(const PagedArgs 
       make_uint2(pack2bf(num.x * inv, num.y * inv), pack2bf(num.z * inv, num.w * inv));
 }
 
+// query rows of a tile.  (max_new is the caller's word; more tokens than that only make more tiles.)
+static int prompt_rows(const PagedArgs& a, int max_new) { return (long long)max_new * (a.hpr / a.kvpr) <= 64 ? 64 : 128; }
+
 // at most as many tiles (of all heads) as this: a sequence's last one is not full
-static long long prompt_tiles(const PagedArgs& a) {
+static long long prompt_tiles(const PagedArgs& a, int bq) {
   const long long rows = (long long)a.rows * (a.hpr / a.kvpr);
-  return std::min((rows + PBQ - 1) / PBQ + a.batch - 1, rows) * a.T * a.kvpr;
+  return std::min((rows + bq - 1) / bq + a.batch - 1, rows) * a.T * a.kvpr;
 }
 
-size_t paged_prompt_workspace_bytes(const PagedArgs& a) {
-  return prompt_tiles(a) > PLINE ? 0 : PLINE * sizeof(PromptJoin) + 2 * PWGS * (size_t)(PBQ * PPR) * sizeof(float);
+size_t paged_prompt_workspace_bytes(const PagedArgs& a, int max_new) {
+  const int bq = prompt_rows(a, max_new);
+  return prompt_tiles(a, bq) > PLINE ? 0 : PLINE * sizeof(PromptJoin) + 2 * PWGS * (size_t)(bq * PPR) * sizeof(float);
 }
 
-hipError_t launch_paged_prompt(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, void* workspace,
-                               hipStream_t s) {
-  const long long tiles = prompt_tiles(a), most = ((long long)a.max_pages * a.page_size / PBK + 2) * 16 + PSTART;   // of a tile
+template <int RG>
+static auto prompt_kernel(int e4m3, int line) {
+  return e4m3 ? (line ? paged_prompt_kernel<true, true, RG> : paged_prompt_kernel<true, false, RG>)
+              : (line ? paged_prompt_kernel<false, true, RG> : paged_prompt_kernel<false, false, RG>);
+}
+
+hipError_t launch_paged_prompt(const PagedArgs& a, int e4m3, int max_new, const bf16_t* q, bf16_t* out, const void* kc, const void* vc,
+                               void* workspace, hipStream_t s) {
+  const int bq = prompt_rows(a, max_new);
+  const long long tiles = prompt_tiles(a, bq), most = ((long long)a.max_pages * a.page_size / PBK + 2) * 16 + PSTART;   // of a tile
   const int line_room = tiles <= PLINE && most >= PLINE_KEYS * 16 && most <= 0x7FFFFFFFLL / tiles ? (int)tiles : 0;
   PromptJoin* joins = reinterpret_cast<PromptJoin*>(workspace);
   float* part = reinterpret_cast<float*>(joins + PLINE);
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)PHD);
-  auto kernel = e4m3 ? (line_room ? paged_prompt_kernel<true, true> : paged_prompt_kernel<true, false>)
-                     : (line_room ? paged_prompt_kernel<false, true> : paged_prompt_kernel<false, false>);
+  auto kernel = bq == 64 ? prompt_kernel<2>(e4m3, line_room) : prompt_kernel<4>(e4m3, line_room);
   const long long wgs = line_room ? std::min<long long>(PWGS, (most * tiles / PLEAST + 8) / 8 * 8) : tiles;
   hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), 0, s, a, q, out, kc, vc, part, joins, scale_log2, line_room);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !line_room) return e;
   if (tiles <= PWGS / 8)                         // many parts of a tile (8 tiles over 52000 keys 82 -> 66 us, 64 over 16384: 79 and 78)
-    hipLaunchKernelGGL(paged_prompt_join_kernel<8>, dim3((unsigned)tiles, PBQ), dim3(256), 0, s, a, part, joins, out);
+    hipLaunchKernelGGL(paged_prompt_join_kernel<8>, dim3((unsigned)tiles, (unsigned)bq), dim3(256), 0, s, a, part, joins, out, bq);
   else
-    hipLaunchKernelGGL(paged_prompt_join_kernel<1>, dim3((unsigned)tiles, PBQ / 8), dim3(256), 0, s, a, part, joins, out);
+    hipLaunchKernelGGL(paged_prompt_join_kernel<1>, dim3((unsigned)tiles, (unsigned)(bq / 8)), dim3(256), 0, s, a, part, joins, out, bq);
   return hipGetLastError();
 }
 

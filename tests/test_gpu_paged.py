@@ -326,3 +326,63 @@ def test_a_batch_that_grows_step_by_step(e4m3):
         P.check_append(c, P.bits(d.q_out), k, v, c.k, c.v)
         c.k, c.v = k, v
         P.check_attn(c, P.bits(d.out), *P.ref_attn(c, q=P.bits(d.q_out)), P.slack(c))
+
+
+# 33 to 64 rows of a key / value head: two waves share 32 rows
+DRAFTS = [
+    (1, 8, 1, [500, 40, 0, 7], [8, 5, 0, 7], 16, False, "phrd"),             # 64, 40 and 56 rows
+    (2, 16, 2, [700, 33, 64, 65, 1], [5, 1, 5, 5, 1], 48, False, "prhd"),
+    (1, 1, 1, [32, 33, 64, 96, 97, 129], [32, 33, 64, 40, 50, 64], 16, False, "phrd"),   # blocks of which one half has no keys
+    (2, 4, 4, [4100, 55], [50, 55], 80, False, "hprd"),                      # the keys of a tile dealt to many workgroups
+    (1, 8, 1, [3001, 500, 8], [8, 6, 1], 32, True, "phrd"),
+    (2, 6, 2, [200, 77, 20], [20, 21, 20], 16, True, "prhd"),                # 60 and 63 rows, groups of 3 heads
+    (8, 64, 8, [(97 * i) % 613 for i in range(50)], [min((97 * i) % 613, 6) for i in range(50)], 16, False, "phrd"),   # 400 tiles
+    (8, 64, 8, [(97 * i) % 613 for i in range(50)], [min((97 * i) % 613, 5) for i in range(50)], 32, True, "phrd"),
+    (1, 2, 1, [2000 * (i % 2) + 25 for i in range(70)], [25 - i % 7 for i in range(70)], 64, False, "phrd"),
+]
+
+
+@pytest.mark.parametrize("T,heads,kv,lens,news,page,e4m3,order", DRAFTS)
+def test_attention_of_drafts(T, heads, kv, lens, news, page, e4m3, order):
+    c = P.make(40, T, heads, kv, lens, news, page, e4m3, order, pad_rows=2)
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    first = P.bits(d.out).copy()
+    P.check_attn(c, first, *P.ref_attn(c), P.slack(c))
+    for _ in range(3):
+        d.out.fill_(-7.0)
+        P.attend(c, d)
+        assert np.array_equal(P.bits(d.out), first)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("hint", [9, 16])
+def test_more_new_tokens_than_max_new_says(hint, e4m3):
+    """Tiles of 64 rows, several of a sequence."""
+    c = P.make(41, 1, 8, 2, [3000, 40, 333, 0, 5], [190, 1, 33, 0, 5], 16, e4m3)
+    c.desc.max_new = hint
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_what_no_query_of_a_draft_sees_does_not_matter(e4m3):
+    """NaN and infinities behind a sequence's length, in pages of nobody and in both halves of a block; a page that is none in either."""
+    lens, new = [6 + 20, 6 + 33, 6 + 90, 2100], 6
+    c = P.make(42, 1, 8, 1, lens, [new] * 4, 16, e4m3)
+    c.table[1, 0], c.table[2, 3], c.table[2, 4], c.table[3, 100] = -1, -1, c.n_pages, 2 ** 31 - 1
+    used = np.zeros((c.n_pages, c.page), dtype=bool)
+    for b, x in enumerate(lens):
+        for t in range(x):
+            if 0 <= c.table[b, t // c.page] < c.n_pages:
+                used[c.table[b, t // c.page], t % c.page] = True
+    for x in (c.k, c.v):
+        w = P.view(c, x)
+        bad = [0x7F, 0xFF] if e4m3 else [0x7FC0, 0xFF80, 0x7F80, 0xFFFF]
+        fill = np.resize(np.array(bad, dtype=x.dtype), w.shape)
+        for page, off in zip(*np.where(~used)):
+            w[:, page, :, off] = fill[:, page, :, off]
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
