@@ -309,7 +309,7 @@ typedef struct caat_paged_desc {
   long long ld_qkv, ld_q; /* elements from row to row of qkv and q; 0: packed.  Ranks lie rows * ld apart */
   long long stride_rank, stride_page, stride_head, stride_row; /* of both caches, in elements, multiples of 16; all 0:
                            [T][n_pages][n_kv_heads / T][page_size][128].  Any order of pages, heads and positions whose 128
-                           channels are contiguous; 16 * stride_row elements must stay below 2 GiB */
+                           channels are contiguous; stride_row at least 128 and below 2^26 */
 } caat_paged_desc;
 
 /*
@@ -327,9 +327,9 @@ int caat_paged_append(const caat_paged_desc* d, const void* qkv, void* q_out, co
 /*
  * Causal attention of the new tokens over the pages of their sequences (their own keys are read from the cache, so they are
  * appended first): out[row of token i of b, head] = sum_t softmax_t(q . k_t / sqrt(128)) v_t over positions
- * t <= lens[b] - n + i.  q [T, rows, hd_r] with rotated queries, out [T, rows, hd_r] packed, which must not overlap q.  A row that sees no key, or whose
- * scores are all minus infinity, is zeros.  Nothing that lies in a page behind its sequence's length takes part, whatever it
- * holds.  workspace: caat_paged_attn_workspace_bytes(d) bytes, which depends neither on the lengths nor on max_pages;
+ * t <= lens[b] - n + i.  q [T, rows, hd_r] with rotated queries, out [T, rows, hd_r] packed, which must not overlap q.  A row
+ * that sees no key, or whose scores are all minus infinity, is zeros.  Nothing that lies in a page behind its sequence's length
+ * takes part, whatever it holds.  workspace: caat_paged_attn_workspace_bytes(d) bytes, which depends neither on the lengths nor on max_pages;
  * nothing in it has to be kept or cleared between calls.
  */
 size_t caat_paged_attn_workspace_bytes(const caat_paged_desc* d);

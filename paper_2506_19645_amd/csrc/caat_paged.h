@@ -38,6 +38,7 @@ __device__ __forceinline__ int wave_sums(int v) {
 }
 
 // The two forms of the attention: caat_paged_few.hip, caat_paged_prompt.hip
+inline bool paged_few_rows(const PagedArgs& a, int max_new) { return (long long)max_new * (a.hpr / a.kvpr) <= 32; }
 bool paged_few_takes(const PagedArgs& a, int max_new);
 size_t paged_few_workspace_bytes(const PagedArgs& a, int max_new);
 hipError_t launch_paged_few(const PagedArgs& a, int e4m3, int max_new, const bf16_t* q, bf16_t* out, const void* kc, const void* vc,

@@ -107,26 +107,32 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
   int units_to = wave_sums(sq.units), work_to = wave_sums(sq.work);
   int units = __builtin_amdgcn_readlane(units_to, 63), total = __builtin_amdgcn_readlane(work_to, 63);
   int chunk_units = lane ? 0 : units, chunk_work = lane ? 0 : total;   // lane k: of chunk k, the first 64 of them
+  bool beyond = (work_to | units_to) < 0;                     // a sum has passed 31 bits (one sequence cannot)
   for (int at = 64; at < a.batch; at += 256) {
     SeqChunk c[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) c[k] = load_seqs(at + 64 * k, 0);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int u = __builtin_amdgcn_readlane(wave_sums(c[k].units), 63), w = __builtin_amdgcn_readlane(wave_sums(c[k].work), 63);
+      const int usums = wave_sums(c[k].units), wsums = wave_sums(c[k].work);
+      const int u = __builtin_amdgcn_readlane(usums, 63), w = __builtin_amdgcn_readlane(wsums, 63);
       units += u;
       total += w;
+      beyond |= (usums | wsums | units | total) < 0;
       if (lane == at / 64 + k) {
         chunk_units = u;
         chunk_work = w;
       }
     }
   }
-  units *= heads;                                // (the host has checked that the line has less than 2^31 places)
-  total *= heads;
   const bool wide = mode == FEW_WG || (mode == FEW_LINE && total >= (long long)units * FWIDE);
   const int start_blocks = mode == FEW_LINE ? (wide ? FSTART * FNW : FSTART) : 0;
-  total += units * start_blocks;
+  // The host has checked that the line has less than 2^31 places.  A list that gives rows to many sequences can make it longer: then
+  // nobody takes any.
+  const long long line = ((long long)units * start_blocks + total) * heads;
+  const bool none = __any(beyond) || line > 0x7FFFFFFF;
+  total = none ? 0 : (int)line;
+  units = none ? 0 : units * heads;
   sq.work += sq.units * start_blocks;
   work_to += units_to * start_blocks;
   const int takers = wide ? gridDim.x : gridDim.x * FNW, taker = wide ? blockIdx.x : wid;
@@ -134,9 +140,7 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
   const int x0 = (int)min((long long)taker * per, (long long)total), x1 = min(total - x0, per) + x0;
   FewJoin join = {};
   if (x0 < x1) {
-    // the sequence of place x0: `base` is where its first unit begins, unit0 the number of that unit.  (A list that gives rows to
-    // many sequences can make the line longer than 31 bits, and what stands here wrong: the checks that follow keep
-    // such a wave inside the buffers.)
+    // the sequence of place x0: `base` is where its first unit begins, unit0 the number of that unit
     int b = a.batch, unit0 = 0, base = 0;
     if (a.batch > 64) {                          // its chunk, or the last of the first 64
       const int own = chunk_work + chunk_units * start_blocks, upto = wave_sums(own), uupto = wave_sums(chunk_units);
@@ -180,7 +184,6 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
       const int unit = base + u * nb;            // place of the unit
       const int to = min(unit + nb, x1);         // and of the stretch's part of it: x .. to - 1
       const int h = (int)((unsigned)u / (unsigned)tiles), tile = u - h * tiles;
-      if (h >= heads) break;                     // (rows given twice, see above)
       const int rank = h / a.kvpr, kvh = h - rank * a.kvpr;
       // its blocks of keys
       int k0 = 0, k1 = nblk;
@@ -575,7 +578,7 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
     }
   }
   if (unit_joins) {                              // the launch has room for unit_joins units
-    for (int i = max(units, 0) + wid * 64 + lane; i < unit_joins; i += gridDim.x * FNW * 64) joins[i].rows = 0;
+    for (int i = units + wid * 64 + lane; i < unit_joins; i += gridDim.x * FNW * 64) joins[i].rows = 0;
   } else if (mode == FEW_LINE && lane == 0) {
     joins[wid] = join;
   }
@@ -666,7 +669,7 @@ static long long few_units(const PagedArgs& a, int nt) {
 // more: 64 sequences of 500 keys 60 / 30).  So does what would not leave the line's places 31 bits.
 bool paged_few_takes(const PagedArgs& a, int max_new) {
   const long long nb = ((long long)a.max_pages * a.page_size + 15) / 16 + FSTART * FNW;
-  return (long long)max_new * (a.hpr / a.kvpr) <= 32 && few_units(a, few_tiles(a, max_new)) <= 0x7FFFFFFFLL / nb;
+  return paged_few_rows(a, max_new) && few_units(a, few_tiles(a, max_new)) <= 0x7FFFFFFFLL / nb;
 }
 
 size_t paged_few_workspace_bytes(const PagedArgs& a, int max_new) {

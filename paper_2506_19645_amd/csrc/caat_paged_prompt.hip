@@ -147,14 +147,20 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
     PromptSeq c = load_seq(lane);
     int own = c.before(c.tiles), incl = wave_sums(own), uincl = wave_sums(c.tiles);
     int total = __builtin_amdgcn_readlane(incl, 63), units = __builtin_amdgcn_readlane(uincl, 63);
+    bool beyond = incl < 0;                      // a sum has passed 31 bits (one sequence cannot)
     for (int at = 64; at < a.batch; at += 64) {
       const PromptSeq d = load_seq(at + lane);
-      total += __builtin_amdgcn_readlane(wave_sums(d.before(d.tiles)), 63);
+      const int sums = wave_sums(d.before(d.tiles));
+      total += __builtin_amdgcn_readlane(sums, 63);
+      beyond |= (sums | total) < 0;
       units += __builtin_amdgcn_readlane(wave_sums(d.tiles), 63);
     }
-    total *= heads;                              // (the host has checked that this is below 2^31)
-    units *= heads;
-    for (int i = max(units, 0) + taker * 256 + tid; i < line_room; i += gridDim.x * 256) joins[i].rows = 0;
+    // The host has checked that the line has less than 2^31 places.  A list that gives rows to many sequences can make it longer: then
+    // nobody takes any.
+    const bool none = __any(beyond) || (long long)total * heads > 0x7FFFFFFF;
+    total = none ? 0 : total * heads;
+    units = none ? 0 : units * heads;
+    for (int i = units + taker * 256 + tid; i < line_room; i += gridDim.x * 256) joins[i].rows = 0;
     per = max((int)((unsigned)(total + gridDim.x - 1) / gridDim.x), PLEAST);
     x = (int)min((long long)taker * per, (long long)total);
     x1 = min(total - x, per) + x;
@@ -178,11 +184,8 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
       base += __builtin_amdgcn_readlane(incl, 63) * heads;
       unit0 += __builtin_amdgcn_readlane(uincl, 63) * heads;
     }
-    // (A list that gives rows to many sequences can make the line longer than 31 bits: then there may be none, or a wrong one.)
-    if (b < 0 || x < base) return;
     const int one = sq.before(sq.tiles);
     h = (int)((unsigned)(x - base) / (unsigned)one);
-    if (h >= heads) return;
     const int r = x - base - h * one;
     for (tile = 0; tile + 64 <= sq.tiles && sq.before(tile + 64) <= r; tile += 64) {}
     tile += __popcll(__ballot(tile + lane < sq.tiles && sq.before(tile + lane) <= r)) - 1;

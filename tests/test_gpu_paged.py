@@ -386,3 +386,22 @@ def test_what_no_query_of_a_draft_sees_does_not_matter(e4m3):
     d = P.on_gpu(c)
     P.attend(c, d)
     P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
+
+
+@pytest.mark.parametrize("new", [1, 16, 30, 90])
+def test_rows_that_everybody_claims(new):
+    """A list that gives all rows to 3000 sequences of 2^24 positions: more work than 31 bits count.  Nothing is written outside
+    the packed rows, and nothing done at length."""
+    import torch
+    c = P.make(43, 1, 2, 1, [new] * 2, [new] * 2, 16, pad_rows=1)
+    batch, columns = 6000, 1 << 10
+    d = P.on_gpu(c)
+    desc = B.paged_desc(T=1, batch=batch, n_heads=2, n_kv_heads=1, rows=c.rows, page_size=1 << 14, n_pages=c.n_pages,
+                        max_pages=columns, max_new=new)
+    rows = torch.tensor([0, c.rows - 1] * (batch // 2) + [0], dtype=torch.int32, device="cuda")
+    lens = torch.full((batch,), 2 ** 31 - 1, dtype=torch.int32, device="cuda")
+    table = torch.full((batch, columns), -1, dtype=torch.int32, device="cuda")
+    ws = torch.full((max(B.paged_attn_workspace_bytes(desc), 1),), 0x7B, dtype=torch.uint8, device="cuda")
+    B.paged_attn(desc, d.q, d.out, rows, lens, table, d.k, d.v, ws)
+    got = P.widen(P.bits(d.out))
+    assert np.all(got[:, -1] == -7.0) and np.all((got == 0.0) | (got == -7.0))
