@@ -37,6 +37,15 @@ __device__ __forceinline__ int wave_sums(int v) {
   return v;
 }
 
+// the product of two rows' eight bf16 values
+__device__ __forceinline__ float dot8(const uint4& a, const uint4& b) {
+  const unsigned x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s += lo_bf(x[i]) * lo_bf(y[i]) + hi_bf(x[i]) * hi_bf(y[i]);
+  return s;
+}
+
 // The two forms of the attention: caat_paged_few.hip, caat_paged_prompt.hip
 inline bool paged_few_rows(const PagedArgs& a, int max_new) { return (long long)max_new * (a.hpr / a.kvpr) <= 32; }
 bool paged_few_takes(const PagedArgs& a, int max_new);

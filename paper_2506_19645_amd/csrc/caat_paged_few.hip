@@ -7,7 +7,8 @@
 // knows).  A wave copies its blocks global -> LDS into two slots that only it reads, waits for its own copies alone, and computes
 // S = K q^T and O^T += V^T P with MFMAs (columns = query rows; most are idle for multi-head attention, but the matrix unit has
 // nothing else to do).  P goes in as a sum of two bf16 values, 16 bits of it; a wave whose sums are not finite
-// (infinity times the second value's zero) repeats its keys with fp32 MFMAs.  A unit inside one stretch is finished there; of
+// (infinity times the second value's zero, or times that of a row that does not see the key) repeats its keys with fp32 MFMAs, and
+// those that some of its rows do not see without.  A unit inside one stretch is finished there; of
 // one that crosses stretches every wave (or, inside it, every workgroup) leaves its sums, maximum and denominator in the
 // workspace, and a second kernel joins them in the order of the keys.
 #include <math.h>
@@ -447,7 +448,11 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
       };
       sweep(std::false_type{});
       wait_vmcnt<0>();                           // the copies past the end write zeros: let them land
-      if constexpr (!E4M3) {
+      // A value that is not finite, times a probability of zero: of the second part, or of a row that does not see its key (one new
+      // token has no such rows).  Then the blocks that every row sees are done again with whole probabilities, and the other keys by
+      // lanes, each for its row and dims.
+      const int cut = max(k0, min(k1, max(min(len - n + tile * ROWS / grp + 1, keys), 0) / KB));
+      if (!E4M3 || cut < k1) {
         bool odd = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -456,9 +461,57 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
 #pragma unroll
             for (int r = 0; r < 4; ++r) odd |= !(fabsf(acc[nt][dt][r]) < INFINITY);
         if (__any(odd)) {
+          const int to_key = min(k1 * KB, keys);
+          k1 = cut;
           start();
-          sweep(std::true_type{});
+          sweep(std::integral_constant<bool, !E4M3>{});
           wait_vmcnt<0>();
+          for (int key = cut * KB; key < to_key; ++key) {
+            const int kcol = key / a.page_size, page = a.table[(long long)b * a.max_pages + kcol];
+            if (page < 0 || page >= a.n_pages) continue;
+            const long long at = (page * a.s_page + (key - kcol * a.page_size) * a.s_row) * ELT;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              float s = 0.0f;
+#pragma unroll
+              for (int t = 0; t < 4; ++t) {
+                uint4 kw;
+                if constexpr (E4M3) {
+                  const uint2 w = *reinterpret_cast<const uint2*>(kh + at + 16 * g + 8 * (t & 1) + 64 * (t >> 1));
+                  kw = make_uint4(fp8_lo(w.x), fp8_hi(w.x), fp8_lo(w.y), fp8_hi(w.y));
+                } else {
+                  kw = *reinterpret_cast<const uint4*>(kh + at + (32 * t + 8 * g) * 2);
+                }
+                s += dot8(kw, __builtin_bit_cast(uint4, qf[nt][t]));
+              }
+              s += __shfl_xor(s, 16, 64);
+              s += __shfl_xor(s, 32, 64);
+              if (key >= lim[nt]) continue;
+              s *= sc_log2;
+              const float m_new = fmaxf(m[nt], s), mb = m_new == -INFINITY ? 0.0f : m_new;
+              const float alpha = __builtin_amdgcn_exp2f(m[nt] - mb), p = __builtin_amdgcn_exp2f(s - mb);
+              m[nt] = m_new;
+              l[nt] = l[nt] * alpha + (g == 0 ? p : 0.0f);
+#pragma unroll
+              for (int t = 0; t < 4; ++t) {
+                uint4 w;                         // dims of acc[2 t] and acc[2 t + 1]: e4m3 in turn, bf16 one after the other
+                if constexpr (E4M3) {
+                  const uint2 c = *reinterpret_cast<const uint2*>(vh + at + 32 * t + 8 * g);
+                  w = make_uint4(fp8_lo(c.x), fp8_hi(c.x), fp8_lo(c.y), fp8_hi(c.y));
+                } else {
+                  const uint2 c = *reinterpret_cast<const uint2*>(vh + at + (32 * t + 4 * g) * 2);
+                  const uint2 d = *reinterpret_cast<const uint2*>(vh + at + (32 * t + 16 + 4 * g) * 2);
+                  w = make_uint4(c.x, c.y, d.x, d.y);
+                }
+                const float v[8] = {lo_bf(w.x), hi_bf(w.x), lo_bf(w.y), hi_bf(w.y), lo_bf(w.z), hi_bf(w.z), lo_bf(w.w), hi_bf(w.w)};
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                  acc[nt][2 * t][r] = acc[nt][2 * t][r] * alpha + p * v[E4M3 ? 2 * r : r];
+                  acc[nt][2 * t + 1][r] = acc[nt][2 * t + 1][r] * alpha + p * v[E4M3 ? 2 * r + 1 : 4 + r];
+                }
+              }
+            }
+          }
         }
       }
 #pragma unroll

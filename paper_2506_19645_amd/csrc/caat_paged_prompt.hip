@@ -75,6 +75,15 @@ __device__ __forceinline__ float pmax3(float a, float b, float c) {
   return d;
 }
 
+__device__ __forceinline__ uint2 widen4(unsigned w) {   // e4m3 codes as bf16 (exact)
+  return make_uint2(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.0f, false)),
+                    __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.0f, true)));
+}
+__device__ __forceinline__ uint4 widen8(const uint2& w) {
+  const uint2 a = widen4(w.x), b = widen4(w.y);
+  return make_uint4(a.x, a.y, b.x, b.y);
+}
+
 // LINE: the workgroup takes a stretch of the line (line_room: tiles that joins has room for), otherwise one tile
 // RG: groups of 32 query rows of a tile.  4: a wave owns a group.  2: two waves share a group, each takes half of every block's keys,
 // and their results meet in LDS; for sequences with at most 64 rows, of which two waves of a tile of 128 would have none (64 heads on
@@ -88,10 +97,9 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
   constexpr int ELT = E4M3 ? 1 : 2;
   constexpr int BQ = 32 * RG;                    // query rows of a tile
   constexpr int KT = RG / 2;                     // tiles of 32 keys of a block that are a wave's
-  __shared__ uint4 smem[4 * PTILE + (E4M3 ? PRAW : 0)];   // K slots 0 and 1, V slots 0 and 1, 16 KB each; e4m3 buffers
+  __shared__ uint4 smem[4 * PTILE + (E4M3 ? PRAW : 1)];   // K slots 0 and 1, V slots 0 and 1, 16 KB each; e4m3 buffers
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = uni(tid >> 6);
-  const int frow = lane & 31, hf = lane >> 5;
   const int rg = wave % RG, part_of = wave / RG;  // group of rows, half of the keys (0 where there is one)
   const int grp = a.hpr / a.kvpr, heads = a.T * a.kvpr;
 
@@ -192,7 +200,14 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
   }
   const float scale0 = scale_log2;
 
+  bool again = false;
   for (bool more = false;; more = true) {        // the tiles of the stretch
+    // What a tile needs is made when it begins: what the compiler keeps from one to the next it keeps in scratch memory (32 heads, 6
+    // prompts 207 us, with this 185; drafts e4m3 37.3 and 29.4).
+    int lane_now = tid & 63;
+    asm volatile("" : "+v"(lane_now));
+    if (!LINE) asm volatile("" : "+s"(h), "+s"(tile), "+s"(b));
+    const int lane = lane_now & 63, frow = lane & 31, hf = lane >> 5;
     const int n = sq.n, first = sq.first, len = sq.len;
     const int rank = h / a.kvpr, kvh = h - rank * a.kvpr;
     const int keys = min(len, cap);
@@ -210,9 +225,13 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
       blk1 = (int)((long long)all_blk * (min(x1, end) - begin) / length);
     }
     const bool begins = x <= begin, all_here = begins && x1 >= end;
-    const int nblk = blk1 - blk0;
+    const int all = blk1 - blk0;
+    // Zero times a value that is not finite is NaN, also for rows that do not see its key.  A tile with such sums is begun again: its
+    // blocks that every row sees as before, the other keys, at most 128 and a block's, by lanes, each for its row and dims.
+    const int cut = max(0, min(all, max(min(len - n + row0 / grp + 1, keys), 0) / PBK - blk0));
+    const int nblk = again ? cut : all;
     const int key0 = blk0 * PBK;
-    if (LINE && more) __syncthreads();                     // everyone is done with the last tile's blocks
+    if (more) __syncthreads();                     // everyone is done with the last tile's blocks
 
     // ---- Q fragments: B operand of S^T = K q^T: lane (row frow, k-half hf) holds q[16 ks + 8 hf .. + 7]
     const int qr = row0 + rg * 32 + frow;
@@ -587,6 +606,60 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
         key_block(blk, sa, sb, std::integral_constant<int, 0>{}, std::true_type{});
       }
     }
+
+    if (again) {
+      for (int kk = cut * PBK; kk < all * PBK; ++kk) {
+        const int key = key0 + kk;
+        if (key >= kv_end) break;
+        if (RG == 2 && (kk >> 5 & 1) != part_of) continue;
+        const int col = key / a.page_size, page = *(const_i_t)(table + col * 4);
+        if ((unsigned)page >= (unsigned)n_pages) continue;
+        const long long at = page * page_bytes + (key - col * a.page_size) * (long long)row_bytes;
+        float s = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < PHD / 16; ++ks) {
+          uint4 w;
+          if constexpr (E4M3) w = widen8(*reinterpret_cast<const uint2*>(kh + at + ks * 16 + hf * 8));
+          else w = *reinterpret_cast<const uint4*>(kh + at + (ks * 16 + hf * 8) * 2);
+          s += dot8(w, *reinterpret_cast<const uint4*>(src + ks * 16));
+        }
+        s += __shfl_xor(s, 32, 64);
+        if (key >= lim) continue;
+        const float m_new = fmaxf(m_run, s), mz = m_new == -INFINITY ? 0.0f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f((m_run - mz) * scale_log2);
+        const float p = lo_bf(pack2bf(__builtin_amdgcn_exp2f((s - mz) * scale_log2), 0.0f));
+        m_run = m_new;
+        l_run = l_run * alpha + (hf == 0 ? p : 0.0f);
+#pragma unroll
+        for (int dt = 0; dt < PHD / 32; ++dt)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int d = dt * 32 + k * 8 + hf * 4;
+            uint2 w;
+            if constexpr (E4M3) w = widen4(*reinterpret_cast<const unsigned*>(vh + at + d));
+            else w = *reinterpret_cast<const uint2*>(vh + at + d * 2);
+            const float v[4] = {lo_bf(w.x), hi_bf(w.x), lo_bf(w.y), hi_bf(w.y)};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) oacc[dt][4 * k + r] = oacc[dt][4 * k + r] * alpha + p * v[r];
+          }
+      }
+    } else if (cut < all) {
+      float odd = 0.0f;                            // NaN where a sum is not finite
+#pragma unroll
+      for (int t = 0; t < PHD / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) odd = __builtin_fmaf(oacc[t][r], 0.0f, odd);
+      const bool wave_odd = __any(odd != odd);
+      int* said = reinterpret_cast<int*>(smem + 4 * PTILE);   // (e4m3: a wave's own buffer, which has been read)
+      constexpr int NEXT = E4M3 ? 256 * 4 : 1;
+      if (lane == 0) said[wave * NEXT] = wave_odd;
+      __syncthreads();
+      if (said[0] | said[NEXT] | said[2 * NEXT] | said[3 * NEXT]) {
+        again = true;
+        continue;
+      }
+    }
+    again = false;
 
     // ---- normalise and store: lane holds out[row][32 dt + 8 (r / 4) + 4 hf + r % 4]
     l_run += __shfl_xor(l_run, 32, 64);

@@ -405,3 +405,39 @@ def test_rows_that_everybody_claims(new):
     B.paged_attn(desc, d.q, d.out, rows, lens, table, d.k, d.v, ws)
     got = P.widen(P.bits(d.out))
     assert np.all(got[:, -1] == -7.0) and np.all((got == 0.0) | (got == -7.0))
+
+
+@pytest.mark.parametrize("new,grp", [(2, 4), (4, 4), (3, 8), (8, 8), (33, 1), (40, 3), (150, 2)])
+@pytest.mark.parametrize("long", [0, 70, 1500])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_what_later_tokens_hold_does_not_matter(new, grp, long, e4m3):
+    """Values and keys of new tokens that are not finite: only the tokens from there on see them."""
+    c = P.make(44, 1, 2 * grp, 2, [long + new, new + 33], [new, new], 16, e4m3)
+    k, v = P.view(c, c.k), P.view(c, c.v)
+    mid, last = new // 2, new - 1
+    nan, inf = (0x7F, 0xFF) if e4m3 else (0x7FC0, 0xFF80)
+    odd = np.zeros((2 * new, 2 * grp, 128), dtype=bool)
+    poison = []
+    for b in range(2):
+        at = lambda i: (c.table[b, (c.lens[b] - new + i) // 16], (c.lens[b] - new + i) % 16)
+        (p0, o0), (p1, o1) = at(mid), at(last)
+        poison += [(p0, 0, o0, 5, nan), (p0, 0, o0, 77, inf), (p0, 1, o0, 100, inf)] + [(p1, 0, o1, x, nan) for x in range(128)]
+        odd[b * new + mid:(b + 1) * new, :grp, [5, 77]] = True
+        odd[b * new + mid:(b + 1) * new, grp:, 100] = True
+        odd[b * new + last, :grp] = True
+        k[0, p1, 1, o1, 3] = nan
+        odd[b * new + last, grp:] = True
+    for p, h, o, x, _ in poison:
+        v[0, p, h, o, x] = 0
+    ref, size = (x.reshape(2 * new, 2 * grp, 128)[~odd] for x in P.ref_attn(c))
+    for p, h, o, x, code in poison:
+        v[0, p, h, o, x] = code
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    first = P.bits(d.out).copy()
+    got = P.widen(first).reshape(2 * new, 2 * grp, 128)
+    assert not np.any(np.isfinite(got[odd]))
+    assert np.all(np.abs(got[~odd] - ref) <= 2.0 ** -8 * np.abs(ref) + P.slack(c) * size)
+    d.out.fill_(-7.0)
+    P.attend(c, d)
+    assert np.array_equal(P.bits(d.out), first)
