@@ -1,6 +1,7 @@
 // Paged key / value cache for gfx950: the new tokens of a ragged batch are rotated and stored to the pages of their sequences,
 // and attend to them.
 #include <math.h>
+#include <algorithm>
 #include "caat_paged.h"
 
 namespace caat {
@@ -172,8 +173,9 @@ hipError_t launch_paged_append(const PagedArgs& a, int e4m3, const bf16_t* qkv, 
 }
 
 size_t paged_attn_workspace_bytes(const PagedArgs& a, int max_new) {
-  // (whichever of the two takes few rows under a table of this width: the prompts' kernel needs less for them)
-  return paged_few_rows(a, max_new) ? paged_few_workspace_bytes(a, max_new) : paged_prompt_workspace_bytes(a, max_new);
+  // whichever of the two takes few rows under a table of this width
+  const size_t bytes = paged_prompt_workspace_bytes(a, max_new);
+  return paged_few_rows(a, max_new) ? std::max(bytes, paged_few_workspace_bytes(a, max_new)) : bytes;
 }
 
 hipError_t launch_paged_attn(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, int max_new,

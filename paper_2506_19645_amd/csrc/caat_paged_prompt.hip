@@ -35,14 +35,21 @@ static constexpr int PRAW = 4 * 256;             // chunks of the waves' e4m3 bu
 static constexpr int PPR = PHD + 4;              // floats of a partial row: 128 sums, maximum, denominator, 2 unused
 static constexpr int PWGS = 512;                 // workgroups that run at a time
 
-// Few tiles (at most PLINE, of all heads) over many keys do not fill the chip, or fill it unevenly: then the tiles of all sequences
-// stand in one line, each as long as its blocks and PSTART more (its start and its results' way), and every workgroup takes an equal
-// stretch.  In us, a tile per workgroup (few tiles: an equal share of its keys) / the line: 216 tiles of a ragged batch with up to 6000
-// keys 76 / 43, 232 with up to 5003 90 / 82, 8 over 52000 57 / 51, 256 of one prompt over 16384 320 / 323; but 520 tiles of two
-// prompts over 8192 keys 270 / 294, and 160 over 900 keys 30 / 38: the line needs PLINE_KEYS blocks of keys too.
+// Few tiles over many keys do not fill the chip, or fill it unevenly: then the tiles of all sequences stand in one line, each as long
+// as its blocks and PSTART more (its start and its results' way), and every workgroup takes an equal stretch.  In us, a tile
+// per workgroup (few tiles: an equal share of its keys) / the line: 216 tiles of a ragged batch with up to 6000 keys 76 / 43, 232
+// with up to 5003 90 / 82, 8 over 52000 57 / 51, 256 of one prompt over 16384 320 / 323; but 520 tiles of two prompts over 8192 keys
+// 270 / 294, and 160 over 900 keys 30 / 38: the line needs PLINE_KEYS blocks of keys too.
+// How even a batch is only the device knows, and its sequences' last tiles are not full; the rule looks at what the rows would fill,
+// at most PLINE tiles (32 heads, 70 new tokens of up to 4000 keys, 12 even sequences 157 / 179, ragged ones 104 / 74, e4m3 107 / 61;
+// 8 of 512 new tokens of up to 4096, more than PLINE when even, ragged 107 / 109, even 305 / 376).  Tiles of 64 rows, of sequences
+// with few new tokens and any number of keys, take the line while its notes have room (64 / 8 heads, 5 new tokens of up to 6000 keys,
+// 64 even sequences 271 / 275, ragged ones 142 / 88, e4m3 131 / 68; 256 of up to 3000 549 / 561, 192 / 174, 162 / 141; the worst, 50
+// even ones, 400 tiles in 512 places, 214 / 243).
 // Places count sixteenths of a block; a tile's length is taken as linear in its number, nb0 blocks the first to nb0 + slope / 16 *
 // number, which is what causality makes it up to roundings.
 static constexpr int PLINE = 384;
+static constexpr int PLINE_ROOM = 4096;          // tiles that have a note
 static constexpr int PLINE_KEYS = 24;
 static constexpr int PSTART = 3 * 16;
 static constexpr int PLEAST = 8 * 16;            // shortest stretch
@@ -811,9 +818,15 @@ static long long prompt_tiles(const PagedArgs& a, int bq) {
   return std::min((rows + bq - 1) / bq + a.batch - 1, rows) * a.T * a.kvpr;
 }
 
+// as many as the line may have, 0: no line
+static int prompt_line(const PagedArgs& a, int bq) {
+  const long long tiles = prompt_tiles(a, bq), full = ((long long)a.rows * (a.hpr / a.kvpr) + bq - 1) / bq * a.T * a.kvpr;
+  return tiles <= PLINE_ROOM && (bq == 64 || full <= PLINE) ? (int)tiles : 0;
+}
+
 size_t paged_prompt_workspace_bytes(const PagedArgs& a, int max_new) {
   const int bq = prompt_rows(a, max_new);
-  return prompt_tiles(a, bq) > PLINE ? 0 : PLINE * sizeof(PromptJoin) + 2 * PWGS * (size_t)(bq * PPR) * sizeof(float);
+  return prompt_line(a, bq) ? PLINE_ROOM * sizeof(PromptJoin) + 2 * PWGS * (size_t)(bq * PPR) * sizeof(float) : 0;
 }
 
 template <int RG>
@@ -826,9 +839,9 @@ hipError_t launch_paged_prompt(const PagedArgs& a, int e4m3, int max_new, const 
                                void* workspace, hipStream_t s) {
   const int bq = prompt_rows(a, max_new);
   const long long tiles = prompt_tiles(a, bq), most = ((long long)a.max_pages * a.page_size / PBK + 2) * 16 + PSTART;   // of a tile
-  const int line_room = tiles <= PLINE && most >= PLINE_KEYS * 16 && most <= 0x7FFFFFFFLL / tiles ? (int)tiles : 0;
+  const int line_room = most >= PLINE_KEYS * 16 && most <= 0x7FFFFFFFLL / tiles ? prompt_line(a, bq) : 0;
   PromptJoin* joins = reinterpret_cast<PromptJoin*>(workspace);
-  float* part = reinterpret_cast<float*>(joins + PLINE);
+  float* part = reinterpret_cast<float*>(joins + PLINE_ROOM);
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)PHD);
   auto kernel = bq == 64 ? prompt_kernel<2>(e4m3, line_room) : prompt_kernel<4>(e4m3, line_room);
   const long long wgs = line_room ? std::min<long long>(PWGS, (most * tiles / PLEAST + 8) / 8 * 8) : tiles;

@@ -441,3 +441,19 @@ def test_what_later_tokens_hold_does_not_matter(new, grp, long, e4m3):
     d.out.fill_(-7.0)
     P.attend(c, d)
     assert np.array_equal(P.bits(d.out), first)
+
+
+@pytest.mark.parametrize("T,heads,kv,new,e4m3", [(8, 64, 8, 5, False), (8, 64, 8, 5, True), (4, 16, 16, 40, False), (8, 64, 8, 9, True), (1, 8, 8, 80, False)])
+def test_a_long_line_of_tiles(T, heads, kv, new, e4m3):
+    """More tiles than workgroups, of many sequences with lengths far apart, free slots among them."""
+    lens = [(397 * i) % 1700 + 1 if i % 7 else 0 for i in range(70)]
+    lens[33] = 3500
+    news = [min(x, 1 + (i * 5) % new) if i % 3 else min(x, new) for i, x in enumerate(lens)]
+    c = P.make(45, T, heads, kv, lens, news, 32, e4m3, pad_rows=1)
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    first = P.bits(d.out).copy()
+    P.check_attn(c, first, *P.ref_attn(c), P.slack(c))
+    d.out.fill_(-7.0)
+    P.attend(c, d)
+    assert np.array_equal(P.bits(d.out), first)
