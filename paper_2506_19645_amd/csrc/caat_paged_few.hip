@@ -717,9 +717,10 @@ static long long few_units(const PagedArgs& a, int nt) {
 }
 
 // More than 32 rows of queries go to the prompts' kernel, whose vector work per score is less (us, here with three and four
-// tiles / there: 64 / 8 heads, 24 sequences of up to 6000 keys, 24 rows 114 / 124, 40 rows 150 / 128, 64 rows 219 / 166; one of 40000
-// 44 / 59, 63 / 61, 71 / 63; in e4m3 the line would lie at 64 rows for long sequences, 123 / 132 and 46 / 58 at 40, but short ones lose
-// more: 64 sequences of 500 keys 60 / 30).  So does what would not leave the line's places 31 bits.
+// tiles / there: 64 / 8 heads, 24 sequences of 6000 keys, 40 rows 150 / 123, 64 rows 219 / 128; one of 40000 63 / 45, 71 / 48; 64 of
+// 500 keys in e4m3, 40 rows, 60 / 22).  Two tiles stay here, whose probabilities have 16 bits and not 8: 32 rows, here / there, 24 of
+// 6000 118 / 121, e4m3 76 / 83, one of 40000 46 / 44, but 64 of 500 42 / 31, 8 of 120 14.1 / 9.0.  What would not leave the line's
+// places 31 bits goes there too.
 bool paged_few_takes(const PagedArgs& a, int max_new) {
   const long long nb = ((long long)a.max_pages * a.page_size + 15) / 16 + FSTART * FNW;
   return paged_few_rows(a, max_new) && few_units(a, few_tiles(a, max_new)) <= 0x7FFFFFFFLL / nb;

@@ -457,3 +457,14 @@ def test_a_long_line_of_tiles(T, heads, kv, new, e4m3):
     d.out.fill_(-7.0)
     P.attend(c, d)
     assert np.array_equal(P.bits(d.out), first)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("batch,keys,new", [(70, 60, 3), (70, 300, 4), (5, 300, 4), (5, 30, 4), (9, 900, 3)])
+def test_drafts_over_short_tables(batch, keys, new, e4m3):
+    """17 to 32 rows of a key / value head, in more and in fewer units than a launch has workgroups."""
+    lens = [keys - (11 * i) % (keys - new) for i in range(batch)]
+    c = P.make(46, 8, 64, 8, lens, [new - i % 2 for i in range(batch)], 16, e4m3, pad_rows=1)
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
