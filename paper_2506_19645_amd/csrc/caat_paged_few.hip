@@ -6,8 +6,9 @@
 // one long and many short sequences fills the chip like an even one, whatever the lengths (which only the device
 // knows).  A wave copies its blocks global -> LDS into two slots that only it reads, waits for its own copies alone, and computes
 // S = K q^T and O^T += V^T P with MFMAs (columns = query rows; most are idle for multi-head attention, but the matrix unit has
-// nothing else to do).  P goes in as a sum of two bf16 values, 16 bits of it; a wave whose sums are not finite
-// (infinity times the second value's zero, or times that of a row that does not see the key) repeats its keys with fp32 MFMAs, and
+// nothing else to do).  P goes in as an exact sum of three bf16 values, as in the contiguous decode (two of them, 16 bits, us: 300 keys
+// of one sequence 10.1 and not 10.4, 64 x 2048 323 and 323, e4m3 63 of up to 8191 49.8 and 50.2); a wave whose sums are not finite
+// (infinity times a part that is zero, or times the zero of a row that does not see the key) repeats its keys with fp32 MFMAs, and
 // those that some of its rows do not see without.  A unit inside one stretch is finished there; of
 // one that crosses stretches every wave (or, inside it, every workgroup) leaves its sums, maximum and denominator in the
 // workspace, and a second kernel joins them in the order of the keys.
@@ -354,8 +355,8 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
                 kf[j][t] = kw[t];
               }
             }
-          // scores of query row r16 of tile nt and keys blk * KB + 16 j + 4 g + i, then their probabilities in two parts
-          unsigned hi[NT][HV][2], lo[NT][HV][2];
+          // scores of query row r16 of tile nt and keys blk * KB + 16 j + 4 g + i, then their probabilities in three parts
+          unsigned hi[NT][HV][2], mid[NT][HV][2], lo[NT][HV][2];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             f32x4_t sc[HV];
@@ -401,7 +402,9 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
               for (int i = 0; i < 2; ++i) {
                 const float p0 = p[j][2 * i], p1 = p[j][2 * i + 1];
                 hi[nt][j][i] = pack2bf(p0, p1);
-                lo[nt][j][i] = pack2bf(p0 - lo_bf(hi[nt][j][i]), p1 - hi_bf(hi[nt][j][i]));
+                const float r0 = p0 - lo_bf(hi[nt][j][i]), r1 = p1 - hi_bf(hi[nt][j][i]);   // exact, as is the next difference
+                mid[nt][j][i] = pack2bf(r0, r1);
+                lo[nt][j][i] = pack2bf(r0 - lo_bf(mid[nt][j][i]), r1 - hi_bf(mid[nt][j][i]));
               }
             if constexpr (decltype(fp32_c)::value) {
 #pragma unroll
@@ -411,16 +414,20 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
                   const unsigned w = i & 2 ? vw[dt].y : vw[dt].x;
                   acc[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(i & 1 ? hi_bf(w) : lo_bf(w), p[0][i], acc[nt][dt], 0, 0, 0);
                 }
-            } else if constexpr (!E4M3) {        // one product takes both parts against the values twice
-              const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, make_uint4(hi[nt][0][0], hi[nt][0][1], lo[nt][0][0], lo[nt][0][1]));
+            } else if constexpr (!E4M3) {        // one product takes the first two parts against the values twice
+              const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, make_uint4(hi[nt][0][0], hi[nt][0][1], mid[nt][0][0], mid[nt][0][1]));
+              const short4_t pl = __builtin_bit_cast(short4_t, make_uint2(lo[nt][0][0], lo[nt][0][1]));
 #pragma unroll
               for (int dt = 0; dt < 8; ++dt) {
                 const bf16x8_t v2 = __builtin_bit_cast(bf16x8_t, make_uint4(vw[dt].x, vw[dt].y, vw[dt].x, vw[dt].y));
                 acc[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v2, pf, acc[nt][dt], 0, 0, 0);
               }
+#pragma unroll
+              for (int dt = 0; dt < 8; ++dt)
+                acc[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4_t, vw[dt]), pl, acc[nt][dt], 0, 0, 0);
             }
           }
-          if constexpr (E4M3) {                  // the 32 keys' first parts, then their second
+          if constexpr (E4M3) {                  // the 32 keys' first parts, their second, their third
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) {     // dims 32 dt + 2 r16 (acc[2 dt]) and + 1
               unsigned ev[4], od[4];
@@ -436,9 +443,12 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
                 const bf16x8_t ph = __builtin_bit_cast(bf16x8_t, make_uint4(hi[nt][0][0], hi[nt][0][1], hi[nt][HV - 1][0], hi[nt][HV - 1][1]));
+                const bf16x8_t pm = __builtin_bit_cast(bf16x8_t, make_uint4(mid[nt][0][0], mid[nt][0][1], mid[nt][HV - 1][0], mid[nt][HV - 1][1]));
                 const bf16x8_t pl = __builtin_bit_cast(bf16x8_t, make_uint4(lo[nt][0][0], lo[nt][0][1], lo[nt][HV - 1][0], lo[nt][HV - 1][1]));
                 acc[nt][2 * dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, ph, acc[nt][2 * dt], 0, 0, 0);
                 acc[nt][2 * dt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vd, ph, acc[nt][2 * dt + 1], 0, 0, 0);
+                acc[nt][2 * dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, pm, acc[nt][2 * dt], 0, 0, 0);
+                acc[nt][2 * dt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vd, pm, acc[nt][2 * dt + 1], 0, 0, 0);
                 acc[nt][2 * dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ve, pl, acc[nt][2 * dt], 0, 0, 0);
                 acc[nt][2 * dt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vd, pl, acc[nt][2 * dt + 1], 0, 0, 0);
               }
@@ -448,7 +458,7 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
       };
       sweep(std::false_type{});
       wait_vmcnt<0>();                           // the copies past the end write zeros: let them land
-      // A value that is not finite, times a probability of zero: of the second part, or of a row that does not see its key (one new
+      // A value that is not finite, times a probability of zero: of a later part, or of a row that does not see its key (one new
       // token has no such rows).  Then the blocks that every row sees are done again with whole probabilities, and the other keys by
       // lanes, each for its row and dims.
       const int cut = max(k0, min(k1, max(min(len - n + tile * ROWS / grp + 1, keys), 0) / KB));
@@ -718,7 +728,7 @@ static long long few_units(const PagedArgs& a, int nt) {
 
 // More than 32 rows of queries go to the prompts' kernel, whose vector work per score is less (us, here with three and four
 // tiles / there: 64 / 8 heads, 24 sequences of 6000 keys, 40 rows 150 / 123, 64 rows 219 / 128; one of 40000 63 / 45, 71 / 48; 64 of
-// 500 keys in e4m3, 40 rows, 60 / 22).  Two tiles stay here, whose probabilities have 16 bits and not 8: 32 rows, here / there, 24 of
+// 500 keys in e4m3, 40 rows, 60 / 22).  Two tiles stay here, whose probabilities are whole and not of 8 bits: 32 rows, here / there, 24 of
 // 6000 118 / 121, e4m3 76 / 83, one of 40000 46 / 44, but 64 of 500 42 / 31, 8 of 120 14.1 / 9.0.  What would not leave the line's
 // places 31 bits goes there too.
 bool paged_few_takes(const PagedArgs& a, int max_new) {

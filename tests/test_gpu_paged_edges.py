@@ -1,0 +1,58 @@
+"""Attention over and append to a paged cache at the edges of what the calls promise: how exact the probabilities are, scores and
+scales far from 1, rows whose scores are all minus infinity, batches of unlike sequences."""
+import numpy as np
+import pytest
+
+from paper_2506_19645_amd import binding as B
+from tests import paged_util as P
+
+pytestmark = pytest.mark.gpu
+
+
+def _codes(x, e4m3):
+    """Values that the cache type holds exactly, as its codes."""
+    if not e4m3:
+        return P.bf16(x)
+    near = np.abs(P._CODES[None, :] - np.asarray(x, dtype=np.float64).reshape(-1, 1))
+    near[:, np.isnan(P._CODES)] = np.inf
+    assert np.all(near.min(axis=1) == 0)
+    return near.argmin(axis=1).astype(np.uint8).reshape(np.shape(x))
+
+
+def _fill(c, b, head, k, v):
+    """Keys and values [positions, 128] of sequence b to its pages, on every rank."""
+    for t in range(len(k)):
+        page, off = c.table[b, t // c.page], t % c.page
+        P.view(c, c.k)[:, page, head, off], P.view(c, c.v)[:, page, head, off] = _codes(k[t], c.e4m3), _codes(v[t], c.e4m3)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("heads", [1, 16, 20])
+@pytest.mark.parametrize("repeat", [1, 20, 300])
+def test_probabilities_are_whole(e4m3, heads, repeat):
+    """Keys of two scores whose weighted values nearly cancel, so that what is left shows the probabilities' own error: less than
+    2^-20 of sum p |v|.  The scores are exact (one product); times 1.44 / sqrt(128), twice rounded, they are 2^-23 * 0.7 off, so
+    their exponentials 2^-23.5 and the instruction's ulp, 2^-23; the sums run near zero, where a key's rounding is at most 2^-22 of
+    it.  Probabilities of 16 bits are 2^-17.8 off here."""
+    c1, c2, a, b, n1, n2 = -1.625, -5.0, 11.0, 14.0, 17, 18
+    block = [(0.0, 0.0)]
+    while n1 + n2:                                       # in turn, so that the sums stay small
+        if n2 >= n1 and n2:
+            block.append((c2, -b)); n2 -= 1
+        else:
+            block.append((c1, a)); n1 -= 1
+    keys = np.zeros((36 * repeat, 2))
+    keys[:] = block * repeat
+    c = P.make(90, 1, heads, 1, [len(keys)], [1], 16, e4m3, scales=False)
+    k, v = np.zeros((len(keys), 128)), np.zeros((len(keys), 128))
+    k[:, 0] = keys[:, 0]
+    v[:, ::2], v[:, 1::2] = keys[:, 1:], -keys[:, 1:] / 2
+    _fill(c, 0, 0, k, v)
+    q = np.zeros((1, 1, heads, 128))
+    q[..., 0] = 1.0
+    c.q = P.bf16(q.reshape(1, 1, -1))
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    ref, size = P.ref_attn(c)
+    got = P.widen(P.bits(d.out))
+    assert np.all(np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -20 * size), np.max(np.abs(got - ref) / size) * 2 ** 20
