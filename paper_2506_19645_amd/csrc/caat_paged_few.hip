@@ -556,7 +556,12 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           if (!row_ok[nt]) continue;
-          const float inv = l[nt] == 0.0f ? 0.0f : vs / l[nt];
+          float inv = vs / l[nt];
+          if (l[nt] == 0.0f) {                   // no key seen, or all scores minus infinity: zeros, whatever the values hold
+            inv = 0.0f;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) acc[nt][dt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+          }
           bf16_t* dst = out + qat[nt] * PHD;
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
@@ -713,6 +718,7 @@ __global__ __launch_bounds__(64) void paged_few_join_kernel(const PagedArgs a, c
       for (int c0 = 0; c0 < count; c0 += 32) take(c0, std::integral_constant<int, 32>{});
     const int qr = j.row0 + r, token = qr / grp, h = j.kvh * grp + (qr - token * grp);
     const float inv = den == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[j.rank * a.kvpr + j.kvh] : 1.0f) / den;
+    if (den == 0.0f) n0 = n1 = 0.0f;
     *reinterpret_cast<unsigned*>(out + (((long long)j.rank * a.rows + j.first + token) * a.hpr + h) * PHD + lane * 2) = pack2bf(n0 * inv, n1 * inv);
   }
 }

@@ -717,7 +717,14 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
         if (hf == 0) *reinterpret_cast<float2*>(o + PHD) = make_float2(m_run * scale_log2, l_run);
       }
     } else if (stores) {
-      const float inv = l_run == 0.0f ? 0.0f : (E4M3 && a.v_scale ? a.v_scale[h] : 1.0f) / l_run;
+      float inv = (E4M3 && a.v_scale ? a.v_scale[h] : 1.0f) / l_run;
+      if (l_run == 0.0f) {                         // no key seen, or all scores minus infinity: zeros, whatever the values hold
+        inv = 0.0f;
+#pragma unroll
+        for (int t = 0; t < PHD / 32; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) oacc[t][r] = 0.0f;
+      }
       bf16_t* o = out + (qrow * a.hpr + head) * PHD;
 #pragma unroll
       for (int dt = 0; dt < PHD / 32; ++dt)
@@ -805,6 +812,7 @@ __global__ __launch_bounds__(256) void paged_prompt_join_kernel(const PagedArgs 
   }
   const int grp = a.hpr / a.kvpr, qr = j.row0 + r, token = qr / grp, h = j.kvh * grp + (qr - token * grp);
   const float inv = den == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[j.rank * a.kvpr + j.kvh] : 1.0f) / den;
+  if (den == 0.0f) num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   *reinterpret_cast<uint2*>(out + (((long long)j.rank * a.rows + j.first + token) * a.hpr + h) * PHD + c) =
       make_uint2(pack2bf(num.x * inv, num.y * inv), pack2bf(num.z * inv, num.w * inv));
 }

@@ -56,3 +56,27 @@ def test_probabilities_are_whole(e4m3, heads, repeat):
     ref, size = P.ref_attn(c)
     got = P.widen(P.bits(d.out))
     assert np.all(np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -20 * size), np.max(np.abs(got - ref) / size) * 2 ** 20
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("new,grp", [(1, 1), (1, 20), (3, 4), (9, 4), (150, 1)])
+@pytest.mark.parametrize("long", [0, 70, 1500])
+def test_scores_of_minus_infinity_alone_make_zeros(e4m3, new, grp, long):
+    """Every score of a row is minus infinity: zeros, also where the values are infinite or NaN."""
+    c = P.make(91, 1, 2 * grp, 2, [long + new, new + 20], [new, new], 16, e4m3)
+    q = c.q.reshape(1, 2 * new, 2 * grp, 128)
+    q[0, :new, :grp, 3] = 0xFF80
+    k, v = P.view(c, c.k), P.view(c, c.v)
+    pages = c.table[0][c.table[0] >= 0]
+    one, nan, inf = (0x38, 0x7F, 0xFF) if e4m3 else (0x3F80, 0x7FC0, 0x7F80)
+    k[0, pages, 0, :, 3] = one
+    was = v[0, pages, 0].copy()
+    v[0, pages, 0] = 0
+    ref, size = P.ref_attn(c)
+    v[0, pages, 0] = was
+    v[0, pages, 0, :, 5], v[0, pages, 0, ::3, 77] = nan, inf
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    got = P.bits(d.out)
+    assert np.all(ref.reshape(1, 2 * new, 2 * grp, 128)[:, :new, :grp] == 0)
+    P.check_attn(c, got, ref, size, P.slack(c))
