@@ -498,6 +498,7 @@ __global__ __launch_bounds__(64 * FNW, 2) void paged_few_kernel(const PagedArgs 
               s += __shfl_xor(s, 32, 64);
               if (key >= lim[nt]) continue;
               s *= sc_log2;
+              asm volatile("" : "+v"(s));        // its rounding, which m_new has too, stays in front of the difference
               const float m_new = fmaxf(m[nt], s), mb = m_new == -INFINITY ? 0.0f : m_new;
               const float alpha = __builtin_amdgcn_exp2f(m[nt] - mb), p = __builtin_amdgcn_exp2f(s - mb);
               m[nt] = m_new;

@@ -509,6 +509,15 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
           const float mz = m_new == -INFINITY ? 0.0f : m_new;   // no key seen so far: nothing is added
           alpha = __builtin_amdgcn_exp2f((m_run - mz) * scale_log2);
           mb = mz * scale_log2;
+          // prob_pair multiplies and subtracts with one rounding, and mb has a rounding of its own: half of 2^32's last place
+          // makes 2^256 of a probability of 1
+          if (__any(fabsf(mb) >= 0x1p24f)) {
+#pragma unroll
+            for (int j = 0; j < KT; ++j)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) scur[j][r] -= mz;
+            mb = 0.0f;
+          }
         } else if (idx >= 2 * KT + 2 && idx < 6 * KT + 2) {
           prob_pair(idx - 2 * KT - 2);
         }

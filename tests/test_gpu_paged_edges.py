@@ -80,3 +80,21 @@ def test_scores_of_minus_infinity_alone_make_zeros(e4m3, new, grp, long):
     got = P.bits(d.out)
     assert np.all(ref.reshape(1, 2 * new, 2 * grp, 128)[:, :new, :grp] == 0)
     P.check_attn(c, got, ref, size, P.slack(c))
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("new,grp", [(1, 1), (3, 4), (9, 4), (40, 1), (150, 2)])
+@pytest.mark.parametrize("long", [0, 70, 1500])
+@pytest.mark.parametrize("power", [13, 15, 18, 30])
+def test_scores_far_from_one(e4m3, new, grp, long, power):
+    """Queries and keys of 2^13 to 2^30: scores whose last place is more than an exponential's range.  The two largest scores of a row
+    are at least 1.6e-5 of the largest apart for these inputs, the fp32 sums 1e-6: one key's value each."""
+    c = P.make(92, 1, 2 * grp, 2, [long + new, new + 33], [new, new], 16, e4m3)
+    c.q = P.bf16(P.widen(c.q) * 2.0 ** power)
+    if e4m3:
+        c.ks = c.ks * 2.0 ** power
+    else:
+        c.k = P.bf16(P.widen(c.k) * 2.0 ** power)
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
