@@ -289,8 +289,8 @@ int caat_block_bwd(const caat_desc* d, const void* const* weights, const void* x
  */
 typedef enum caat_cache {
   CAAT_CACHE_BF16 = 0,
-  CAAT_CACHE_E4M3 = 1   /* OCP e4m3 codes of value / scale, one fp32 scale per (rank, key / value head) and cache; rounded to
-                           nearest even, beyond +-448 the largest code, NaN stays NaN */
+  CAAT_CACHE_E4M3 = 1   /* OCP e4m3 codes of value / scale (the fp32 quotient), one fp32 scale per (rank, key / value head) and
+                           cache; rounded to nearest even, beyond +-448 the largest code, NaN stays NaN */
 } caat_cache;
 
 typedef struct caat_paged_desc {

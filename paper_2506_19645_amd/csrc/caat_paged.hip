@@ -45,6 +45,20 @@ __device__ __forceinline__ int seq_of_row(const PagedArgs& a, int row, int& firs
 }
 
 __device__ __forceinline__ float e4m3_clamp(float x) { return x != x ? x : fminf(fmaxf(x, -448.0f), 448.0f); }
+// Quotients by s, rounded to nearest in fp32: by its significand, behind a shift by its exponent, so that any s does.  What the
+// product with the rounded reciprocal lacks is exact in fp32, and its share goes to it with one rounding (Markstein, 1990); the product
+// alone moves values off the middle of two codes.  Beyond the codes' range only that they are beyond.  (us, the product / this / the
+// compiler's division: 7047 rows of 32 heads 55.3 / 55.5 / 72, 512 rows 7.9 / 8.5 / 9.8.)
+struct Divisor {
+  float m, r;
+  int e;
+  __device__ __forceinline__ explicit Divisor(float s) : m(__builtin_amdgcn_frexp_mantf(s)), e(-__builtin_amdgcn_frexp_expf(s)) { r = 1.0f / m; }
+  __device__ __forceinline__ float quotient(float x) const {
+    x = ldexpf(x, e);
+    const float q = __builtin_amdgcn_fmed3f(x * r, -480.0f, 480.0f);   // (an infinite one would leave infinity less infinity)
+    return __builtin_fmaf(__builtin_fmaf(-q, m, x), r, q);
+  }
+};
 // eight values to eight e4m3 codes
 __device__ __forceinline__ uint2 pack_e4m3(const float* v) {
   uint2 w;
@@ -127,21 +141,25 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const PagedArgs a, co
       const uint4 vlo = take<STREAM>(src + a.kvpr * PHD), vhi = take<STREAM>(src + a.kvpr * PHD + 64);
       const long long at = rank * a.s_rank + slot + kvh * a.s_head + grp * 8;
       if constexpr (E4M3) {
-        const float ki = a.k_scale ? 1.0f / a.k_scale[rank * a.kvpr + kvh] : 1.0f, vi = a.v_scale ? 1.0f / a.v_scale[rank * a.kvpr + kvh] : 1.0f;
-        const unsigned vw[8] = {vlo.x, vlo.y, vlo.z, vlo.w, vhi.x, vhi.y, vhi.z, vhi.w};
-        float v[16];
+        unsigned char *k8 = (unsigned char*)kc + at, *v8 = (unsigned char*)vc + at;
+        const Divisor ks(a.k_scale ? a.k_scale[rank * a.kvpr + kvh] : 1.0f), vs(a.v_scale ? a.v_scale[rank * a.kvpr + kvh] : 1.0f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          y1[e] *= ki;
-          y2[e] *= ki;
-          v[2 * e] = lo_bf(vw[e]) * vi;
-          v[2 * e + 1] = hi_bf(vw[e]) * vi;
+          y1[e] = ks.quotient(y1[e]);
+          y2[e] = ks.quotient(y2[e]);
         }
-        unsigned char *k8 = (unsigned char*)kc + at, *v8 = (unsigned char*)vc + at;
         *reinterpret_cast<uint2*>(k8) = pack_e4m3(y1);
         *reinterpret_cast<uint2*>(k8 + 64) = pack_e4m3(y2);
-        *reinterpret_cast<uint2*>(v8) = pack_e4m3(v);
-        *reinterpret_cast<uint2*>(v8 + 64) = pack_e4m3(v + 8);
+        const unsigned vw[8] = {vlo.x, vlo.y, vlo.z, vlo.w, vhi.x, vhi.y, vhi.z, vhi.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          y1[2 * e] = vs.quotient(lo_bf(vw[e]));
+          y1[2 * e + 1] = vs.quotient(hi_bf(vw[e]));
+          y2[2 * e] = vs.quotient(lo_bf(vw[4 + e]));
+          y2[2 * e + 1] = vs.quotient(hi_bf(vw[4 + e]));
+        }
+        *reinterpret_cast<uint2*>(v8) = pack_e4m3(y1);
+        *reinterpret_cast<uint2*>(v8 + 64) = pack_e4m3(y2);
       } else {
         put<STREAM>((bf16_t*)vc + at, vlo);
         put<STREAM>((bf16_t*)vc + at + 64, vhi);

@@ -98,3 +98,33 @@ def test_scores_far_from_one(e4m3, new, grp, long, power):
     d = P.on_gpu(c)
     P.attend(c, d)
     P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
+
+
+def _nearest_codes(x):
+    """e4m3 values nearest to x, halves to the even code, saturating."""
+    x = np.clip(np.asarray(x, dtype=np.float64), -448, 448)
+    grid = P._CODES[:0x7F]                               # the non-negative codes run upwards
+    at = np.searchsorted(grid, np.abs(x)).clip(1, len(grid) - 1)
+    lo, hi = grid[at - 1], grid[at]
+    up = (np.abs(x) - lo > hi - np.abs(x)) | ((np.abs(x) - lo == hi - np.abs(x)) & (at % 2 == 0))
+    return np.copysign(np.where(up, hi, lo), x)
+
+
+@pytest.mark.parametrize("scale", [7.0, 7.0 / 512, 3.0, 25.0 / 1024, 2.0 ** -130, 3 * 2.0 ** -149, 2.0 ** 100])
+def test_codes_are_of_the_quotient(scale):
+    """Values in the middle of two codes times scales that are no power of two, and scales whose reciprocal is none of fp32's: the
+    code is that of value / scale.  Position 0, so that keys are stored as they come."""
+    c = P.make(93, 1, 1, 1, [1], [1], 16, True, scales=False)
+    x = np.zeros(128)
+    m = np.array([17, 19, 21, 23, 25, 27, 29, 31, 16, 18, 3, 5, 448, 449, 464, 480], dtype=np.float64)
+    for i in range(8):
+        x[i * 16:(i + 1) * 16] = m * 2.0 ** (i - 6) * (-1) ** i
+    x[15::16] = 0.0
+    want = P.bf16(x * scale)                             # rounded to bf16 where the product has more bits
+    c.qkv[0, 0, 128:256], c.qkv[0, 0, 256:] = want, want
+    c.ks[:], c.vs[:] = scale, scale
+    d = P.on_gpu(c)
+    P.append(c, d)
+    codes = _nearest_codes(np.float32(P.widen(want) / scale))
+    for got in (d.k, d.v):
+        assert np.array_equal(P.decode(P.view(c, P.bits(got))[0, c.table[0, 0], 0, 0], True), codes)
