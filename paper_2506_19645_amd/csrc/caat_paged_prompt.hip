@@ -251,7 +251,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(const PagedArgs a,
     const bf16_t* src = q + (row_ok ? qrow * a.ld_q + head * PHD : 0) + hf * 8;   // rows of nobody: any row, not stored
 #pragma unroll
     for (int ks = 0; ks < PHD / 16; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(src + ks * 16);
-    scale_log2 = E4M3 && a.k_scale ? scale0 * a.k_scale[h] : scale0;
+    scale_log2 = E4M3 && a.k_scale ? fmaxf(scale0 * a.k_scale[h], 0x1p-149f) : scale0;   // (not 0, for minus infinity's sake)
 
     f32x16_t oacc[PHD / 32];
 #pragma unroll

@@ -128,3 +128,16 @@ def test_codes_are_of_the_quotient(scale):
     codes = _nearest_codes(np.float32(P.widen(want) / scale))
     for got in (d.k, d.v):
         assert np.array_equal(P.decode(P.view(c, P.bits(got))[0, c.table[0, 0], 0, 0], True), codes)
+
+
+@pytest.mark.parametrize("new,grp", [(1, 1), (3, 4), (9, 4), (40, 1), (150, 2)])
+@pytest.mark.parametrize("long", [0, 70, 1500])
+@pytest.mark.parametrize("scale", [2.0 ** -149, 2.0 ** -126, 2.0 ** -60, 2.0 ** 100])
+def test_scales_of_keys_far_from_one(new, grp, long, scale):
+    """Any positive scale.  With the small ones all keys that are seen weigh the same; with 2^100 one key takes all, by a gap of 1.4e-5
+    of the largest score for these inputs."""
+    c = P.make(94, 1, 2 * grp, 2, [long + new, new + 33], [new, new], 16, True)
+    c.ks[:] = scale
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
