@@ -328,9 +328,10 @@ int caat_paged_append(const caat_paged_desc* d, const void* qkv, void* q_out, co
  * Causal attention of the new tokens over the pages of their sequences (their own keys are read from the cache, so they are
  * appended first): out[row of token i of b, head] = sum_t softmax_t(q . k_t / sqrt(128)) v_t over positions
  * t <= lens[b] - n + i.  q [T, rows, hd_r] with rotated queries, out [T, rows, hd_r] packed, which must not overlap q.  A row
- * that sees no key, or whose scores are all minus infinity, is zeros, whatever the values hold.  Nothing that lies in a page behind its sequence's length,
- * or belongs to a later new token, takes part, whatever it holds.  workspace: caat_paged_attn_workspace_bytes(d) bytes, which
- * depends neither on the lengths nor on max_pages; nothing in it has to be kept or cleared between calls.
+ * that sees no key, or whose scores are all minus infinity, is zeros, whatever the values hold.  Nothing that lies in a page
+ * behind its sequence's length, or belongs to a later new token, takes part, whatever it holds.
+ *   workspace: caat_paged_attn_workspace_bytes(d) bytes; nothing in it has to be kept or cleared between calls.  The size depends on
+ *   the heads and max_new alone and never falls when max_new grows: one workspace, sized for the most new tokens, serves every call.
  */
 size_t caat_paged_attn_workspace_bytes(const caat_paged_desc* d);
 int caat_paged_attn(const caat_paged_desc* d, const void* q, void* out, const int* row_start, const int* lens,

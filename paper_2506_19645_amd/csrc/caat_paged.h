@@ -47,7 +47,8 @@ __device__ __forceinline__ float dot8(const uint4& a, const uint4& b) {
 }
 
 // The two forms of the attention: caat_paged_few.hip, caat_paged_prompt.hip
-inline bool paged_few_rows(const PagedArgs& a, int max_new) { return (long long)max_new * (a.hpr / a.kvpr) <= 32; }
+static constexpr int PFEW_ROWS = 32;             // the first one's share: (token, head of the group) rows of a sequence
+inline bool paged_few_rows(const PagedArgs& a, int max_new) { return (long long)max_new * (a.hpr / a.kvpr) <= PFEW_ROWS; }
 bool paged_few_takes(const PagedArgs& a, int max_new);
 size_t paged_few_workspace_bytes(const PagedArgs& a, int max_new);
 hipError_t launch_paged_few(const PagedArgs& a, int e4m3, int max_new, const bf16_t* q, bf16_t* out, const void* kc, const void* vc,

@@ -190,10 +190,11 @@ hipError_t launch_paged_append(const PagedArgs& a, int e4m3, const bf16_t* qkv, 
   return hipGetLastError();
 }
 
+// The most that calls with as many new tokens or fewer take, whatever their rows, sequences and tables: a program sizes it once.
 size_t paged_attn_workspace_bytes(const PagedArgs& a, int max_new) {
-  // whichever of the two takes few rows under a table of this width
+  const int few = std::min(max_new, PFEW_ROWS / (a.hpr / a.kvpr));   // the most that the few tokens' kernel is given
   const size_t bytes = paged_prompt_workspace_bytes(a, max_new);
-  return paged_few_rows(a, max_new) ? std::max(bytes, paged_few_workspace_bytes(a, max_new)) : bytes;
+  return few > 0 ? std::max(bytes, paged_few_workspace_bytes(a, few)) : bytes;
 }
 
 hipError_t launch_paged_attn(const PagedArgs& a, int e4m3, const bf16_t* q, bf16_t* out, const void* kc, const void* vc, int max_new,

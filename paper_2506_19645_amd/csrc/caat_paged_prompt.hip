@@ -842,8 +842,7 @@ static int prompt_line(const PagedArgs& a, int bq) {
 }
 
 size_t paged_prompt_workspace_bytes(const PagedArgs& a, int max_new) {
-  const int bq = prompt_rows(a, max_new);
-  return prompt_line(a, bq) ? PLINE_ROOM * sizeof(PromptJoin) + 2 * PWGS * (size_t)(bq * PPR) * sizeof(float) : 0;
+  return PLINE_ROOM * sizeof(PromptJoin) + 2 * PWGS * (size_t)(prompt_rows(a, max_new) * PPR) * sizeof(float);   // of the line
 }
 
 template <int RG>
