@@ -284,8 +284,9 @@ int caat_block_bwd(const caat_desc* d, const void* const* weights, const void* x
  * checked there: a sequence whose rows are not inside 0 .. rows (or end before they begin) has none, a negative length is
  * none, a table entry outside 0 .. n_pages - 1, or a position at or behind max_pages * page_size, is no page: nothing is
  * written there, and its keys are not seen.  A page may stand in the tables of several sequences (a common beginning), but
- * no row may belong to two sequences, nor two tokens of one call be appended to the same place: what such rows and
- * places get is undefined.  Rows that belong to no sequence are left as they are.
+ * two tokens of one call must not be appended to the same place: what it gets is undefined.  Nor must a row belong to two sequences:
+ * with such a list nothing is read or written outside what the call is given, but all that it writes is undefined, other rows'
+ * too.  Rows that belong to no sequence are left as they are.
  */
 typedef enum caat_cache {
   CAAT_CACHE_BF16 = 0,
@@ -303,8 +304,13 @@ typedef struct caat_paged_desc {
   int max_pages;        /* columns of page_table; max_pages * page_size at most 2^30 */
   long long n_pages;    /* pages of a rank's pool */
   long long rows;       /* token rows per rank of qkv, q and out; at most 2^23, and (rows / 128 + batch + 1) * n_heads as well */
-  int max_new;          /* the most new tokens a sequence has in these calls: chooses the kernel, results do not depend on it
-                           beyond their rounding */
+  int max_new;          /* the most new tokens a sequence has in these calls: chooses the attention's kernel, one for all sequences;
+                           results do not depend on it beyond their rounding.  Up to 32 / (n_heads / n_kv_heads), probabilities
+                           are kept whole and the keys are shared out evenly (while 2 * n_kv_heads * batch * (max_pages * page_size
+                           / 16 + 12) is below 2^31).  Beyond, they are rounded to bf16, as in
+                           CAAT_LAYER_PREFILL, and every sequence takes whole tiles of 64 or 128 (token, head) rows: single tokens
+                           beside prompts are served better by a call of their own, over a part of the batch (row_start + b,
+                           lens + b, page_table + b * max_pages), for which the others' rows belong to nobody */
   float rope_base;      /* caat_paged_append: > 0 */
   long long ld_qkv, ld_q; /* elements from row to row of qkv and q; 0: packed.  Ranks lie rows * ld apart */
   long long stride_rank, stride_page, stride_head, stride_row; /* of both caches, in elements, multiples of 16; all 0:

@@ -141,3 +141,60 @@ def test_scales_of_keys_far_from_one(new, grp, long, scale):
     d = P.on_gpu(c)
     P.attend(c, d)
     P.check_attn(c, P.bits(d.out), *P.ref_attn(c), P.slack(c))
+
+
+# Relative 2-norm of the outputs' error over N(0, 1) queries, keys and values: a probability's rounding to bf16 and the output's own are
+# at most half a step each, spread evenly over it, 2^-8 / sqrt(3); of independent values their squares add up to (2^-8)^2 * 2 / 3.
+WHOLE = 2.0 ** -8
+
+
+def check_norm(c, got_bits, ref):
+    own = ~np.isnan(ref)
+    err = P.widen(got_bits)[:, :c.rows][own] - ref[own]
+    assert np.linalg.norm(err) <= WHOLE * np.linalg.norm(ref[own]), np.linalg.norm(err) / np.linalg.norm(ref[own])
+
+
+@pytest.mark.parametrize("T,heads,kv,lens,news,page,e4m3", [
+    (8, 32, 32, [2500, 33], [1600, 1], 16, False),           # 416 full tiles and more: each its own workgroup
+    (8, 32, 32, [2500, 33], [1600, 1], 64, True),
+    (8, 64, 8, [1900, 400, 1500, 1], [700, 90, 1, 1], 48, False),    # 404
+    (8, 64, 8, [900, 1, 30, 2900], [820, 1, 2, 1], 16, True),        # the longest sequence last, one new token
+])
+def test_prompts_without_a_line(T, heads, kv, lens, news, page, e4m3):
+    """More full tiles than share a line, over more than a thousand keys, single tokens and drafts among the prompts."""
+    c = P.make(98, T, heads, kv, lens, news, page, e4m3, pad_rows=3)
+    d = P.on_gpu(c)
+    P.attend(c, d)
+    ref, size = P.ref_attn(c)
+    P.check_attn(c, P.bits(d.out), ref, size, P.slack(c))
+    check_norm(c, P.bits(d.out), ref)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("T,heads,kv", [(2, 8, 2), (4, 8, 8)])
+def test_single_tokens_and_prompts_in_two_calls(T, heads, kv, e4m3):
+    """The sequences of a batch whose first have single tokens and whose last have prompts, in a call each over the same buffers: the
+    rows of the other call's sequences are nobody's and stay, and the single tokens have whole probabilities."""
+    lens, news = [3000, 1, 77, 0, 640, 300, 210], [1, 1, 1, 0, 2, 150, 210]
+    c = P.make(99, T, heads, kv, lens, news, 32, e4m3, pad_rows=2)
+    few = 5
+    def part(b0, b1):
+        return B.paged_desc(T=T, batch=b1 - b0, n_heads=heads, n_kv_heads=kv, rows=c.rows, page_size=32, n_pages=c.n_pages,
+                            max_pages=c.table.shape[1], max_new=max(news[b0:b1]), cache_type=c.desc.cache_type)
+    d, e = P.on_gpu(c), P.on_gpu(c)
+    P.append(c, e)
+    ref, size = P.ref_attn(c)
+    for b0, b1 in ((0, few), (few, 7)):
+        d.out.fill_(-7.0)
+        pg = part(b0, b1)
+        lists = (d.row_start[b0:b1 + 1].clone(), d.lens[b0:b1].clone(), d.table[b0:b1].clone())
+        B.paged_append(pg, d.qkv, d.q_out, *lists, d.k, d.v, d.ks, d.vs)
+        c2 = P.on_gpu(c)                                     # the caches as they were: what ref_attn looks at
+        B.paged_attn(pg, c2.q, d.out, *lists, c2.k, c2.v, c2.ws, c2.ks, c2.vs)
+        r0, r1 = int(c.row_start[b0]), int(c.row_start[b1])
+        mine = np.full(ref.shape, np.nan)
+        mine[:, r0:r1] = ref[:, r0:r1]
+        P.check_attn(c, P.bits(d.out), mine, size, P.FEW if b0 == 0 else P.MANY)
+        check_norm(c, P.bits(d.out), mine)
+    for x in ("q_out", "k", "v"):                            # both appends together: the one call's
+        assert np.array_equal(P.bits(getattr(d, x)), P.bits(getattr(e, x)))
