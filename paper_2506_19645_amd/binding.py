@@ -303,10 +303,52 @@ def paged_desc(T: int, batch: int, n_heads: int, rows: int, page_size: int, n_pa
                            stride_head=strides[2], stride_row=strides[3])
 
 
+_int32 = _float32 = None   # torch's types, once a tensor has come
+
+
+def _learn_types() -> None:
+    global _int32, _float32
+    import torch
+    _int32, _float32 = torch.int32, torch.float32
+
+
+def _int32_ptr(t) -> Optional[int]:
+    """Device pointer of a contiguous int32 tensor."""
+    if t is None or type(t) is int:
+        return t
+    if _int32 is None:
+        _learn_types()
+    if t.dtype is not _int32 or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("expected a contiguous CUDA tensor of int32, not of %s" % t.dtype)
+    return t.data_ptr()
+
+
+def _float32_ptr(t) -> Optional[int]:
+    if t is None or type(t) is int:
+        return t
+    if _int32 is None:
+        _learn_types()
+    if t.dtype is not _float32 or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("expected a contiguous CUDA tensor of float32, not of %s" % t.dtype)
+    return t.data_ptr()
+
+
+def _sized_ptr(t, itemsize: int) -> Optional[int]:
+    """Device pointer of a contiguous tensor of values of this size."""
+    if t is None or type(t) is int:
+        return t
+    if t.element_size() != itemsize:
+        raise ValueError("expected values of %d bytes, not %d" % (itemsize, t.element_size()))
+    return _ptr(t)
+
+
 def paged_append(desc: caat_paged_desc, qkv, q_out, row_start, lens, page_table, k_cache, v_cache, k_scale=None, v_scale=None,
                  stream=None, check: bool = True) -> int:
-    st = lib().caat_paged_append(C.byref(desc), _ptr(qkv), _ptr(q_out), _ptr(row_start), _ptr(lens), _ptr(page_table),
-                                 _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _stream(stream))
+    """row_start, lens and page_table are int32."""
+    size = 1 if desc.cache_type == CACHE_E4M3 else 2
+    st = lib().caat_paged_append(C.byref(desc), _sized_ptr(qkv, 2), _sized_ptr(q_out, 2), _int32_ptr(row_start),
+                                 _int32_ptr(lens), _int32_ptr(page_table), _sized_ptr(k_cache, size),
+                                 _sized_ptr(v_cache, size), _float32_ptr(k_scale), _float32_ptr(v_scale), _stream(stream))
     if check:
         _check(st, "caat_paged_append")
     return st
@@ -318,10 +360,12 @@ def paged_attn_workspace_bytes(desc: caat_paged_desc) -> int:
 
 def paged_attn(desc: caat_paged_desc, q, out, row_start, lens, page_table, k_cache, v_cache, workspace, k_scale=None,
                v_scale=None, stream=None, check: bool = True) -> int:
+    """row_start, lens and page_table are int32."""
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    st = lib().caat_paged_attn(C.byref(desc), _ptr(q), _ptr(out), _ptr(row_start), _ptr(lens), _ptr(page_table),
-                               _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(workspace), ws_bytes,
-                               _stream(stream))
+    size = 1 if desc.cache_type == CACHE_E4M3 else 2
+    st = lib().caat_paged_attn(C.byref(desc), _sized_ptr(q, 2), _ptr(out), _int32_ptr(row_start), _int32_ptr(lens),
+                               _int32_ptr(page_table), _sized_ptr(k_cache, size), _sized_ptr(v_cache, size),
+                               _float32_ptr(k_scale), _float32_ptr(v_scale), _ptr(workspace), ws_bytes, _stream(stream))
     if check:
         _check(st, "caat_paged_attn")
     return st
@@ -333,10 +377,13 @@ def paged_layer_workspace_bytes(desc: caat_desc, pages: caat_paged_desc) -> int:
 
 def paged_layer_fwd(desc: caat_desc, pages: caat_paged_desc, weights: Sequence, r, r_out, row_start, lens, page_table, k_cache,
                     v_cache, workspace, k_scale=None, v_scale=None, stream=None, check: bool = True) -> int:
+    """row_start, lens and page_table are int32."""
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    st = lib().caat_paged_layer_fwd(C.byref(desc), C.byref(pages), _ptr_array(weights), _ptr(r), _ptr(r_out), _ptr(row_start),
-                                    _ptr(lens), _ptr(page_table), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
-                                    _ptr(workspace), ws_bytes, _stream(stream))
+    size = 1 if pages.cache_type == CACHE_E4M3 else 2
+    st = lib().caat_paged_layer_fwd(C.byref(desc), C.byref(pages), _ptr_array(weights), _ptr(r), _ptr(r_out), _int32_ptr(row_start),
+                                    _int32_ptr(lens), _int32_ptr(page_table), _sized_ptr(k_cache, size),
+                                    _sized_ptr(v_cache, size), _float32_ptr(k_scale), _float32_ptr(v_scale), _ptr(workspace),
+                                    ws_bytes, _stream(stream))
     if check:
         _check(st, "caat_paged_layer_fwd")
     return st
