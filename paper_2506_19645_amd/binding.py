@@ -333,22 +333,46 @@ def _float32_ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
-def _sized_ptr(t, itemsize: int) -> Optional[int]:
-    """Device pointer of a contiguous tensor of values of this size."""
-    if t is None or type(t) is int:
-        return t
+def _view_ptr(t, itemsize: int, strides) -> int:
+    """Device pointer of values of this size in a tensor that is contiguous, or has these strides, in elements, and the last
+    dimension's 1."""
     if t.element_size() != itemsize:
         raise ValueError("expected values of %d bytes, not %d" % (itemsize, t.element_size()))
+    if not t.is_contiguous():
+        want = strides + (1,)
+        if not t.is_cuda or t.dim() != len(want) or any(n > 1 and s != w for n, s, w in zip(t.shape, t.stride(), want)):
+            raise ValueError("expected a contiguous CUDA tensor, or one with strides %s" % (want,))
+        return t.data_ptr()
     return _ptr(t)
+
+
+def _rows_ptr(desc: caat_paged_desc, t, ld: str) -> Optional[int]:
+    """Device pointer of bf16 [rank][row][channel] whose rows are desc's `ld` apart."""
+    if t is None or type(t) is int:
+        return t
+    if t.element_size() == 2 and t.is_contiguous() and t.is_cuda:
+        return t.data_ptr()
+    ld = getattr(desc, ld)
+    return _view_ptr(t, 2, (desc.rows * ld, ld))
+
+
+def _cache_ptr(desc: caat_paged_desc, t, itemsize: int) -> Optional[int]:
+    """Device pointer of a cache [rank][page][head][position][channel]."""
+    if t is None or type(t) is int:
+        return t
+    if t.element_size() == itemsize and t.is_contiguous() and t.is_cuda:
+        return t.data_ptr()
+    return _view_ptr(t, itemsize, (desc.stride_rank, desc.stride_page, desc.stride_head, desc.stride_row))
 
 
 def paged_append(desc: caat_paged_desc, qkv, q_out, row_start, lens, page_table, k_cache, v_cache, k_scale=None, v_scale=None,
                  stream=None, check: bool = True) -> int:
-    """row_start, lens and page_table are int32."""
+    """qkv and q_out [rank][row][channel] and the caches [rank][page][head][position][channel] may be views that have desc's strides;
+    row_start, lens and page_table are int32."""
     size = 1 if desc.cache_type == CACHE_E4M3 else 2
-    st = lib().caat_paged_append(C.byref(desc), _sized_ptr(qkv, 2), _sized_ptr(q_out, 2), _int32_ptr(row_start),
-                                 _int32_ptr(lens), _int32_ptr(page_table), _sized_ptr(k_cache, size),
-                                 _sized_ptr(v_cache, size), _float32_ptr(k_scale), _float32_ptr(v_scale), _stream(stream))
+    st = lib().caat_paged_append(C.byref(desc), _rows_ptr(desc, qkv, "ld_qkv"), _rows_ptr(desc, q_out, "ld_q"), _int32_ptr(row_start),
+                                 _int32_ptr(lens), _int32_ptr(page_table), _cache_ptr(desc, k_cache, size),
+                                 _cache_ptr(desc, v_cache, size), _float32_ptr(k_scale), _float32_ptr(v_scale), _stream(stream))
     if check:
         _check(st, "caat_paged_append")
     return st
@@ -360,11 +384,12 @@ def paged_attn_workspace_bytes(desc: caat_paged_desc) -> int:
 
 def paged_attn(desc: caat_paged_desc, q, out, row_start, lens, page_table, k_cache, v_cache, workspace, k_scale=None,
                v_scale=None, stream=None, check: bool = True) -> int:
-    """row_start, lens and page_table are int32."""
+    """q [rank][row][channel] and the caches [rank][page][head][position][channel] may be views that have desc's strides; row_start, lens
+    and page_table are int32."""
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     size = 1 if desc.cache_type == CACHE_E4M3 else 2
-    st = lib().caat_paged_attn(C.byref(desc), _sized_ptr(q, 2), _ptr(out), _int32_ptr(row_start), _int32_ptr(lens),
-                               _int32_ptr(page_table), _sized_ptr(k_cache, size), _sized_ptr(v_cache, size),
+    st = lib().caat_paged_attn(C.byref(desc), _rows_ptr(desc, q, "ld_q"), _ptr(out), _int32_ptr(row_start), _int32_ptr(lens),
+                               _int32_ptr(page_table), _cache_ptr(desc, k_cache, size), _cache_ptr(desc, v_cache, size),
                                _float32_ptr(k_scale), _float32_ptr(v_scale), _ptr(workspace), ws_bytes, _stream(stream))
     if check:
         _check(st, "caat_paged_attn")
@@ -377,12 +402,13 @@ def paged_layer_workspace_bytes(desc: caat_desc, pages: caat_paged_desc) -> int:
 
 def paged_layer_fwd(desc: caat_desc, pages: caat_paged_desc, weights: Sequence, r, r_out, row_start, lens, page_table, k_cache,
                     v_cache, workspace, k_scale=None, v_scale=None, stream=None, check: bool = True) -> int:
-    """row_start, lens and page_table are int32."""
+    """The caches [rank][page][head][position][channel] may be views that have pages' strides; row_start, lens and page_table are
+    int32."""
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     size = 1 if pages.cache_type == CACHE_E4M3 else 2
     st = lib().caat_paged_layer_fwd(C.byref(desc), C.byref(pages), _ptr_array(weights), _ptr(r), _ptr(r_out), _int32_ptr(row_start),
-                                    _int32_ptr(lens), _int32_ptr(page_table), _sized_ptr(k_cache, size),
-                                    _sized_ptr(v_cache, size), _float32_ptr(k_scale), _float32_ptr(v_scale), _ptr(workspace),
+                                    _int32_ptr(lens), _int32_ptr(page_table), _cache_ptr(pages, k_cache, size),
+                                    _cache_ptr(pages, v_cache, size), _float32_ptr(k_scale), _float32_ptr(v_scale), _ptr(workspace),
                                     ws_bytes, _stream(stream))
     if check:
         _check(st, "caat_paged_layer_fwd")

@@ -198,3 +198,24 @@ def test_single_tokens_and_prompts_in_two_calls(T, heads, kv, e4m3):
         check_norm(c, P.bits(d.out), mine)
     for x in ("q_out", "k", "v"):                            # both appends together: the one call's
         assert np.array_equal(P.bits(getattr(d, x)), P.bits(getattr(e, x)))
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_views_of_one_allocation(e4m3):
+    """Keys and values of a page one after the other in one pool, q inside qkv's rows: the bits of tensors of their own."""
+    import torch
+    c = P.make(100, 2, 8, 4, [100, 33, 7], [30, 1, 7], 48, e4m3)
+    d, e = P.on_gpu(c), P.on_gpu(c)
+    P.append(c, d)
+    P.attend(c, d, q=d.q_out)
+    T, pages, kvpr, page = e.k.shape[:4]
+    pool = torch.stack((e.k, e.v), dim=2)                    # [T][pages][2][heads][page][128]
+    k, v = pool[:, :, 0], pool[:, :, 1]
+    qw = (c.hpr + 2 * c.kvpr) * 128
+    desc = B.paged_desc(T=2, batch=3, n_heads=8, n_kv_heads=4, rows=c.rows, page_size=48, n_pages=c.n_pages, max_pages=c.table.shape[1],
+                        max_new=30, cache_type=c.desc.cache_type, ld_q=qw, strides=k.stride()[:4])
+    q = e.qkv[:, :, :c.hpr * 128]
+    B.paged_append(desc, e.qkv, e.qkv, e.row_start, e.lens, e.table, k, v, e.ks, e.vs)
+    B.paged_attn(desc, q, e.out, e.row_start, e.lens, e.table, k, v, e.ws, e.ks, e.vs)
+    for got, want in ((e.out, d.out), (q.contiguous(), d.q_out), (k.contiguous(), d.k), (v.contiguous(), d.v)):
+        assert np.array_equal(P.bits(got), P.bits(want))

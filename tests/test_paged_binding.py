@@ -56,6 +56,17 @@ def _refusing(e4m3=False, **kw):
                                     cache_type=B.CACHE_E4M3 if e4m3 else B.CACHE_BF16), **kw))
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_views_of_a_pool_are_taken(e4m3):
+    """Keys and values interleaved in one allocation, and queries inside wider rows, are what the descriptor's strides are for."""
+    k, v = (Tensor(1 if e4m3 else 2, shape=POOL, strides=STRIDES + (1,)) for _ in range(2))
+    for call in calls(_refusing(e4m3), k=k, v=v, ks=FP32 if e4m3 else None, row_start=None):
+        assert call() == B.EINVAL
+    q = Tensor(shape=(2, 3, 512), strides=(3 * 1536, 1536, 1))
+    append, attend, _ = calls(_refusing(ld_q=1536, ld_qkv=1536), q=q)
+    assert append() == B.EINVAL and attend() == B.EINVAL
+
+
 @pytest.mark.parametrize("name,bad", [
     ("row_start", Tensor(8, False)), ("lens", Tensor(8, False)), ("table", Tensor(8, False)), ("lens", FP32), ("table", Tensor(2, False)),
     ("table", Tensor(4, False, (2, 3), (7, 1))), ("ks", Tensor(2)), ("vs", Tensor(8)), ("ks", INT), ("k", Tensor(4)), ("v", Tensor(1)),
