@@ -94,3 +94,15 @@ def test_rows_that_the_descriptor_does_not_describe_are_refused(bad):
     for call in (append, attend):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("there", [False, True])
+def test_the_current_stream_with_and_without_torchs_shortcut(monkeypatch, there):
+    """The shortcut to the stream's handle is no public name of torch: without it the public one serves."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: type("Stream", (), {"cuda_stream": 77}))
+    if there:
+        monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 50 + device, raising=False)
+    else:
+        monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    assert B._stream(None) == (53 if there else 77) and B._stream(5) == 5
