@@ -7,6 +7,10 @@
 // (S^T = K q^T, 32x32x16 MFMAs), so that a lane owns one query row and the exponentiated score registers, rounded to bf16, are the
 // k-slices of the second product; V comes through the LDS transpose read.  The body is software-pipelined inside a wave: the
 // score MFMAs of block b + 1 are issued one per step between the softmax arithmetic of block b.
+// Probabilities are rounded to bf16, as the contiguous prompt's are, and the row sums take them so: 2^-8 of a weight at most, a relative
+// error of 2.0e-3 in place of 1.6e-3 over 2048 keys, most of both the output's own rounding.  What more bits would cost (us, one value /
+// two / three): 4 x 2048 tokens, 32 heads 186 / 237; 512 of 16384 in e4m3 298 / 390; 5 new tokens, 24 ragged of up to 6000 36.7 / 38.0 /
+// 39.3, 24 of 6000 123 / - / 129, e4m3 86 / - / 105.
 // K and V blocks (double buffered, chunk-swizzled) come from the pages directly, 16 keys of one page at a time; the table's
 // entries are read two blocks ahead of their use through the scalar cache.  An e4m3 block lands as it is in a buffer of
 // each wave's own and is widened to bf16 on its way into the tile, once per workgroup and not once per wave.
