@@ -47,8 +47,9 @@ __device__ __forceinline__ int seq_of_row(const PagedArgs& a, int row, int& firs
 __device__ __forceinline__ float e4m3_clamp(float x) { return x != x ? x : fminf(fmaxf(x, -448.0f), 448.0f); }
 // Quotients by s, rounded to nearest in fp32: by its significand, behind a shift by its exponent, so that any s does.  What the
 // product with the rounded reciprocal lacks is exact in fp32, and its share goes to it with one rounding (Markstein, 1990); the product
-// alone moves values off the middle of two codes.  Beyond the codes' range only that they are beyond.  (us, the product / this / the
-// compiler's division: 7047 rows of 32 heads 55.3 / 55.5 / 72, 512 rows 7.9 / 8.5 / 9.8.)
+// alone moves values off the middle of two codes.  Beyond the codes' range only that they are beyond.  (us, the product / this, kernel
+// alone: 7047 rows of 32 heads 55.6 / 53.6, 512 rows 7.3 / 7.9, 127 rows of 64 / 8 heads 5.6 / 6.0; calls with the compiler's division
+// 7047 rows 72 and not 55, 512 rows 9.8 and not 7.9.)
 struct Divisor {
   float m, r;
   int e;
@@ -115,6 +116,12 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const PagedArgs a, co
     const int rank = u / per, rem = u - rank * per;
     const int head = rem >> 3, grp = rem & 7;
     const bf16_t* src = qkv + ((long long)rank * a.rows + row) * ld_qkv + head * PHD + grp * 8;
+    const bool is_k = head >= a.hpr;
+    float ks = 1.0f, vs = 1.0f;
+    if constexpr (E4M3) {                        // on their way with the row's values (7047 rows of 32 heads 57.9 -> 53.6 us)
+      if (is_k && a.k_scale) ks = a.k_scale[rank * a.kvpr + head - a.hpr];
+      if (is_k && a.v_scale) vs = a.v_scale[rank * a.kvpr + head - a.hpr];
+    }
     const uint4 lo = take<STREAM>(src), hi = take<STREAM>(src + 64);
     const unsigned lw[4] = {lo.x, lo.y, lo.z, lo.w}, hw[4] = {hi.x, hi.y, hi.z, hi.w};
     float y1[8], y2[8];
@@ -125,7 +132,6 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const PagedArgs a, co
       y1[e] = x1 * cs - x2 * sn;
       y2[e] = x2 * cs + x1 * sn;
     }
-    const bool is_k = head >= a.hpr;
     if (!is_k || !E4M3) {
       const uint4 r1 = make_uint4(pack2bf(y1[0], y1[1]), pack2bf(y1[2], y1[3]), pack2bf(y1[4], y1[5]), pack2bf(y1[6], y1[7]));
       const uint4 r2 = make_uint4(pack2bf(y2[0], y2[1]), pack2bf(y2[2], y2[3]), pack2bf(y2[4], y2[5]), pack2bf(y2[6], y2[7]));
@@ -142,21 +148,21 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const PagedArgs a, co
       const long long at = rank * a.s_rank + slot + kvh * a.s_head + grp * 8;
       if constexpr (E4M3) {
         unsigned char *k8 = (unsigned char*)kc + at, *v8 = (unsigned char*)vc + at;
-        const Divisor ks(a.k_scale ? a.k_scale[rank * a.kvpr + kvh] : 1.0f), vs(a.v_scale ? a.v_scale[rank * a.kvpr + kvh] : 1.0f);
+        const Divisor by_ks(ks), by_vs(vs);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          y1[e] = ks.quotient(y1[e]);
-          y2[e] = ks.quotient(y2[e]);
+          y1[e] = by_ks.quotient(y1[e]);
+          y2[e] = by_ks.quotient(y2[e]);
         }
         *reinterpret_cast<uint2*>(k8) = pack_e4m3(y1);
         *reinterpret_cast<uint2*>(k8 + 64) = pack_e4m3(y2);
         const unsigned vw[8] = {vlo.x, vlo.y, vlo.z, vlo.w, vhi.x, vhi.y, vhi.z, vhi.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          y1[2 * e] = vs.quotient(lo_bf(vw[e]));
-          y1[2 * e + 1] = vs.quotient(hi_bf(vw[e]));
-          y2[2 * e] = vs.quotient(lo_bf(vw[4 + e]));
-          y2[2 * e + 1] = vs.quotient(hi_bf(vw[4 + e]));
+          y1[2 * e] = by_vs.quotient(lo_bf(vw[e]));
+          y1[2 * e + 1] = by_vs.quotient(hi_bf(vw[e]));
+          y2[2 * e] = by_vs.quotient(lo_bf(vw[4 + e]));
+          y2[2 * e + 1] = by_vs.quotient(hi_bf(vw[4 + e]));
         }
         *reinterpret_cast<uint2*>(v8) = pack_e4m3(y1);
         *reinterpret_cast<uint2*>(v8 + 64) = pack_e4m3(y2);
