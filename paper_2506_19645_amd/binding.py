@@ -315,7 +315,7 @@ def _learn_types() -> None:
 
 def _int32_ptr(t) -> Optional[int]:
     """Device pointer of a contiguous int32 tensor."""
-    if t is None or type(t) is int:
+    if t is None or isinstance(t, int):
         return t
     if _int32 is None:
         _learn_types()
@@ -325,7 +325,7 @@ def _int32_ptr(t) -> Optional[int]:
 
 
 def _float32_ptr(t) -> Optional[int]:
-    if t is None or type(t) is int:
+    if t is None or isinstance(t, int):
         return t
     if _int32 is None:
         _learn_types()
@@ -349,7 +349,7 @@ def _view_ptr(t, itemsize: int, strides) -> int:
 
 def _rows_ptr(desc: caat_paged_desc, t, ld: str) -> Optional[int]:
     """Device pointer of bf16 [rank][row][channel] whose rows are desc's `ld` apart."""
-    if t is None or type(t) is int:
+    if t is None or isinstance(t, int):
         return t
     if t.element_size() == 2 and t.is_contiguous() and t.is_cuda:
         return t.data_ptr()
@@ -359,7 +359,7 @@ def _rows_ptr(desc: caat_paged_desc, t, ld: str) -> Optional[int]:
 
 def _cache_ptr(desc: caat_paged_desc, t, itemsize: int) -> Optional[int]:
     """Device pointer of a cache [rank][page][head][position][channel]."""
-    if t is None or type(t) is int:
+    if t is None or isinstance(t, int):
         return t
     if t.element_size() == itemsize and t.is_contiguous() and t.is_cuda:
         return t.data_ptr()

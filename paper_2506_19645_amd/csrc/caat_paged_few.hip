@@ -65,8 +65,8 @@ enum FewMode { FEW_LINE = 0, FEW_WAVE = 1, FEW_WG = 2 };
 // A unit's start (its queries' and pages' way, the first block's, its results) takes a wave about as long as FSTART blocks: they
 // stand in the line in front of the unit's own.  Where units have FWIDE blocks and more on average, a stretch belongs to a workgroup,
 // whose waves take a quarter of a unit's blocks each and join their results in LDS, so that a quarter as many go through the
-// workspace (us, a wave's stretches / a workgroup's: 32 heads, 63 x 2048 keys 368 / 322, 128 x 512 170 / 169, 128 x 256 88 / 94;
-// 64 / 8 heads, 48 of up to 16384 145 / 140; 58 of 19, 16 heads 20 / 32).
+// workspace (us, a wave's stretches / a workgroup's: 32 heads, 63 x 2048 keys 370 / 327, 128 x 512 171 / 173, 128 x 256 89 / 100;
+// 64 / 8 heads, 48 of up to 16384 145 / 144; 58 of 19 under a table of 640, 16 heads 13.7 / 15.6).
 static constexpr int FSTART = 3;
 static constexpr int FWIDE = 24;
 
@@ -736,7 +736,7 @@ static long long few_units(const PagedArgs& a, int nt) {
 // More than 32 rows of queries go to the prompts' kernel, whose vector work per score is less (us, here with three and four
 // tiles / there: 64 / 8 heads, 24 sequences of 6000 keys, 40 rows 150 / 123, 64 rows 219 / 128; one of 40000 63 / 45, 71 / 48; 64 of
 // 500 keys in e4m3, 40 rows, 60 / 22).  Two tiles stay here, whose probabilities are whole and not of 8 bits: 32 rows, here / there, 24 of
-// 6000 118 / 121, e4m3 76 / 83, one of 40000 46 / 44, but 64 of 500 42 / 31, 8 of 120 14.1 / 9.0.  What would not leave the line's
+// 6000 119 / 121, e4m3 78 / 83, one of 40000 47 / 44, but 64 of 500 43 / 31, 8 of 120 13.8 / 9.2.  What would not leave the line's
 // places 31 bits goes there too.
 bool paged_few_takes(const PagedArgs& a, int max_new) {
   const long long nb = ((long long)a.max_pages * a.page_size + 15) / 16 + FSTART * FNW;
@@ -754,10 +754,10 @@ hipError_t launch_paged_few(const PagedArgs& a, int e4m3, int max_new, const bf1
   const int nt = few_tiles(a, max_new);
   const long long units = few_units(a, nt);
   // A cache (as wide as its table) of so few keys that a workgroup does them in the time of a second kernel's launch, while the launch
-  // has one for every unit; one of so few that a wave does.  In us, 32 heads, bf16: one sequence of 300 keys 13.2 in the line, 9.1
-  // a workgroup each; 128 sequences of 60 keys 28.1 in the line, 26.1 a wave each, of 120 keys 45.7 and 43.6; one sequence of 60
-  // keys 8.6 a wave each, 7.6 a workgroup.  Two tiles take a workgroup's joins longer: 31 sequences of 14 keys, 32 rows each, 8.6 a
-  // wave each, 11.9 a workgroup, of 120 keys 17.0 and 14.9.
+  // has one for every unit; one of so few that a wave does.  In us, 32 heads, bf16: one sequence of 300 keys 12.2 in the line, 10.8
+  // a workgroup each; 128 sequences of 60 keys 29.5 in the line, 27.1 a wave each, of 120 keys 46.9 and 45.0; one sequence of 60
+  // keys 9.7 a wave each, 7.9 a workgroup.  Two tiles take a workgroup's joins longer: 31 sequences of 14 keys, 32 rows each, 9.7 a
+  // wave each, 12.5 a workgroup, of 120 keys 17.9 and 14.8.
   const int mode = nb <= 4 && nt > 1 ? FEW_WAVE : nb <= 8 * FNW && units <= FMAX_WGS ? FEW_WG : nb <= 8 ? FEW_WAVE : FEW_LINE;
   const int least = mode == FEW_LINE ? 2 : 1;    // both slots of a wave (one of 3001 keys, 64 / 8 heads, 1 / 2 / 4 blocks: 16.0 / 13.7 / 15.0 us)
   const long long most = mode == FEW_WG ? units * FNW : mode == FEW_WAVE ? units : units * (nb + FSTART * FNW);

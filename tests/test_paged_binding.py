@@ -106,3 +106,19 @@ def test_the_current_stream_with_and_without_torchs_shortcut(monkeypatch, there)
     else:
         monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
     assert B._stream(None) == (53 if there else 77) and B._stream(5) == 5
+
+
+@pytest.mark.parametrize("T,heads,kv", [(2, 8, 8), (8, 64, 8)])
+def test_one_workspace_serves_smaller_batches_of_the_layer(T, heads, kv):
+    """The layer's size never falls when rows or new tokens grow."""
+    from paper_2506_19645_amd import inputs as I
+    for max_new in (1, 5, 300):
+        last = 0
+        for rows in (1, 2, 7, 64, 65, 100, 512, 1536, 4096, 20000):
+            cfg = I.BlockConfig("dec", I.KIND_DECODE, I.NORM_RMSNORM, h=1024, T=T, p=0.5, batch=rows, seq=1, ffn=1024, n_heads=heads,
+                                head_dim=128, n_kv_heads=kv)
+            pages = B.paged_desc(T=T, batch=3, n_heads=heads, n_kv_heads=kv, rows=rows, max_new=max_new, page_size=16, n_pages=99,
+                                 max_pages=50)
+            size = B.paged_layer_workspace_bytes(B.make_desc(cfg), pages)
+            assert size >= last and size > 0
+            last = size
